@@ -425,6 +425,110 @@ int value_cache_append(const kl_value_cache* cache, const void* values,
                        const int32_t* lengths_before, int B, int T, void* stream);
 
 /*
+ * Scored attention: the keyless attention with the score changes and masks that
+ * trained models use beside the causal one. For query row i and value row j of a
+ * sequence, with z = scale <q~_i, v_j>,
+ *   x_ij = cap tanh(z / cap) - slopes[h] |i - j|      (cap 0: z itself)
+ * and row i sees the value rows first[b, i] <= j < last[b, i]. The descriptor lives
+ * in host memory; its pointers are device pointers owned by the caller.
+ *   cap     >= 0 and finite; 0 for no cap
+ *   slopes  [H] fp32, any finite values, or NULL for no bias
+ *   first   [B, N] int32, or NULL for 0
+ *   last    [B, N] int32, or NULL for i + 1 (causal) or N (not causal); when it is
+ *           given, causal is not read
+ * Packed documents: first = the start of the token's document, last = i + 1.
+ * A prefix mask: last = max(i + 1, end of the document's prefix). Padding: first =
+ * last. Both are clamped to [0, N]; a row with first >= last sees nothing. What a row
+ * does not see never reaches it, whatever those values hold (infinities and NaN
+ * included); a value that is not finite makes the columns it lies in NaN for every
+ * row that sees it.
+ */
+typedef struct {
+  float cap;
+  const float* slopes;
+  const int32_t* first;
+  const int32_t* last;
+  int causal;
+} kl_scoring;
+
+/*
+ * keyless_scored_forward - keyless_attention_forward with these scores:
+ *   q_routed [B, N, H, d_head], v [B, N, G, d_head], out [B, N, H, d_head]
+ *   lse      [B, H, N] fp32, or NULL: ln sum_j exp(x_ij) over the rows that row i sees
+ *   out_f32  [B, N, H, d_head] fp32, or NULL: the output before its rounding
+ * Tensors are 16-byte aligned (lse 4). A row that sees nothing has a zero output and
+ * lse = -inf. fp32 sums and softmax statistics; bf16 weights are rounded to bf16 for
+ * the weighted sum (the products run on the matrix cores), their sum is not.
+ * scale and errors as for keyless_prefill; at most 2^31 - 1 elements per sequence and
+ * tensor row counts B * N up to 2^30.
+ */
+int keyless_scored_forward(const void* q_routed, const void* v, const kl_scoring* scoring, int B,
+                           int N, int H, int G, int d_head, float scale, kl_dtype dtype, void* out,
+                           float* lse, float* out_f32, void* stream);
+
+/*
+ * keyless_scored_backward - gradients of keyless_scored_forward with respect to the
+ * routed queries and the values, given dL/dO (cap, slopes and masks are constants):
+ *   dx = P * (dO V^T - rowsum(dO * O)),  P = exp(x - lse)
+ *   dz = dx (1 - tanh^2(z / cap))                        (cap 0: dx itself)
+ *   dq_routed = scale dz V,   dv = P^T dO + scale dz^T Q~ (summed over a group's heads)
+ * out, lse and out_f32 (or NULL) as keyless_scored_forward wrote them for the same
+ * arguments; other tensors and the row sums as for keyless_attention_backward. A
+ * query row that sees nothing has a zero gradient and gives none. Deterministic (no
+ * atomics). ws, ws_bytes: keyless_scored_backward_workspace_size(...) bytes, 16-byte
+ * aligned; calls that run at the same time must not share it.
+ */
+int keyless_scored_backward(const void* q_routed, const void* v, const void* out,
+                            const float* out_f32, const void* dout, const float* lse,
+                            const kl_scoring* scoring, int B, int N, int H, int G, int d_head,
+                            float scale, kl_dtype dtype, void* dq_routed, void* dv, void* ws,
+                            size_t ws_bytes, void* stream);
+size_t keyless_scored_backward_workspace_size(int B, int N, int H, int G, int d_head,
+                                              kl_dtype dtype);
+
+/*
+ * keyless_tree_decode - attention of T drafted tokens per sequence over a value-only
+ * cache in which their values already lie (value_cache_append with these T rows):
+ * drafted token t of sequence b, whose value is row n + t (n = lengths_before[b]),
+ * sees rows 0 .. n - 1 and the drafted rows u with bit u of tree[b, t] set.
+ *   q_routed  [B, T, H, d_head], cache dtype; T is 1 to 64
+ *   tree      [B, T] 64-bit words on the device (bits T and above are not read); a
+ *             token of a tree has the bits of its ancestors and its own. NULL: a
+ *             chain, token t sees drafted rows 0 .. t (T = 1: one decode step)
+ *   cap, slopes, scale  as for keyless_scored_forward, with positions n + depth, a
+ *             token's depth being the number of bits in its word beside its own, so
+ *             that two branches' tokens of one depth are at one position
+ *   out       [B, T, H, d_head]
+ *   ws, ws_bytes  keyless_tree_decode_workspace_size(...) bytes, 16-byte aligned (may
+ *             be 0, then ws may be NULL); calls that run at the same time must not
+ *             share it
+ * H / G takes any value. n is clamped to [0, capacity]; drafted rows past the
+ * capacity and blocks outside the cache are not seen; a token that sees nothing has
+ * a zero row. A row that no token sees is never used, and a row that some tokens do
+ * not see never reaches those, whatever it holds. Results do not depend on how the
+ * work is split beyond rounding, and are the same from run to run.
+ */
+int keyless_tree_decode(const void* q_routed, const kl_value_cache* cache,
+                        const int32_t* lengths_before, const uint64_t* tree, int B, int T, int H,
+                        float cap, const float* slopes, float scale, void* out, void* ws,
+                        size_t ws_bytes, void* stream);
+size_t keyless_tree_decode_workspace_size(const kl_value_cache* cache, int B, int T, int H);
+
+/*
+ * value_cache_keep - the accepted drafted rows move up: for every sequence and group,
+ * row n + k := row n + path[b, k] for k < kept[b] (n = lengths_before[b]), all rows
+ * read before any is written, so that rows 0 .. n + kept[b] - 1 are the sequence.
+ *   path  [B, T] int32 on the device, drafted rows in the order they are kept (entries
+ *         at and past kept[b] are not read); T is 0 to 64
+ *   kept  [B] int32 on the device, clamped to [0, T]
+ * An entry outside [0, T), and a row outside the capacity or in a block outside the
+ * cache, is not moved. Other rows stay as they are; lengths are the caller's.
+ * Sequences of a paged cache must not share the blocks of their drafted rows.
+ */
+int value_cache_keep(const kl_value_cache* cache, const int32_t* lengths_before,
+                     const int32_t* path, const int32_t* kept, int B, int T, void* stream);
+
+/*
  * standard_decode - the comparison baseline: standard attention of Eq. 1 for
  * one new query per sequence over a key cache and a value cache with the same
  * layout as `v_cache` (scores <q, k_i>, weights applied to v_i). Same tiling,

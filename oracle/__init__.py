@@ -9,4 +9,4 @@ Pins (tests that tie it to facts outside itself) are in tests/test_oracle_*.py.
 Every function here has at least one; none is "parity unpinned".
 """
 
-from . import keyless  # noqa: F401
+from . import keyless, scored  # noqa: F401

@@ -31,6 +31,8 @@ EXPORTS = (
     "keyless_weight_gradients", "keyless_weight_gradients_workspace_size",
     "keyless_decode_project", "keyless_decode", "keyless_decode_chunked", "keyless_decode_workspace_size",
     "keyless_decode_append", "keyless_decode_noalloc",
+    "keyless_scored_forward", "keyless_scored_backward", "keyless_scored_backward_workspace_size",
+    "keyless_tree_decode", "keyless_tree_decode_workspace_size", "value_cache_keep",
     "value_cache_append", "standard_decode", "standard_decode_chunked",
     "keyless_set_kernel_timer", "keyless_probe_read", "keyless_probe_mfma",
     "keyless_last_error", "keyless_version",
@@ -52,6 +54,13 @@ class KLValueCache(ctypes.Structure):
     ]
 
 
+class KLScoring(ctypes.Structure):
+    _fields_ = [
+        ("cap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("first", ctypes.c_void_p),
+        ("last", ctypes.c_void_p), ("causal", ctypes.c_int),
+    ]
+
+
 _lib = None
 
 
@@ -67,6 +76,7 @@ def load(path: str = LIB_PATH):
     lib = ctypes.CDLL(path)
     vp, i, f, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
     cp = ctypes.POINTER(KLValueCache)
+    scp = ctypes.POINTER(KLScoring)
     sig = {
         "keyless_fold_routing": (i, [vp, vp, i, i, i, i, vp, vp]),
         "keyless_prefill": (i, [vp, vp, vp, vp, i, i, i, i, i, i, i, f, i, vp, vp, vp, vp, sz, vp]),
@@ -95,6 +105,13 @@ def load(path: str = LIB_PATH):
         "keyless_weight_gradients": (i, [vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, vp, vp, vp,
                                          vp, vp, sz, vp]),
         "keyless_weight_gradients_workspace_size": (sz, [i, i, i, i, i, i, i]),
+        "keyless_scored_forward": (i, [vp, vp, scp, i, i, i, i, i, f, i, vp, vp, vp, vp]),
+        "keyless_scored_backward": (i, [vp, vp, vp, vp, vp, vp, scp, i, i, i, i, i, f, i, vp, vp, vp,
+                                        sz, vp]),
+        "keyless_scored_backward_workspace_size": (sz, [i, i, i, i, i, i]),
+        "keyless_tree_decode": (i, [vp, cp, vp, vp, i, i, i, f, vp, f, vp, vp, sz, vp]),
+        "keyless_tree_decode_workspace_size": (sz, [cp, i, i, i]),
+        "value_cache_keep": (i, [cp, vp, vp, vp, i, i, vp]),
         "value_cache_append": (i, [cp, vp, vp, i, i, vp]),
         "standard_decode": (i, [vp, cp, cp, vp, i, i, f, vp, vp, sz, vp]),
         "standard_decode_chunked": (i, [vp, cp, cp, vp, i, i, f, vp, vp, sz, i, vp]),
@@ -536,3 +553,146 @@ def keyless_decode_noalloc(q_routed: torch.Tensor, cache: ValueCache, lengths: t
     _check(_lib.keyless_decode_noalloc(_ptr(q_routed), cache.ref, _ptr(lengths), B, H, scale,
                                        _ptr(out), _stream(q_routed)))
     return out
+
+
+def _like(t, shape, dtype, dev, what):
+    """t as an argument: None, or a tensor of this shape and type on that device."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{what} is on another device than the first argument")
+    return _ptr(t)
+
+
+def _call(dev: int, fn, *args):
+    """fn on that device's current stream, whichever device is current."""
+    if dev == torch._C._cuda_getDevice():
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev)))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev)))
+
+
+class Scoring:
+    """How keyless_scored_forward and _backward score: a tanh cap (0: none), a distance
+    bias (slopes [H] fp32), and the value rows [first, last) that each row sees (int32
+    [B, N]; without first from row 0, without last to row i + 1 when causal, else to the
+    end). Packed documents: first is the start of the token's document; a prefix
+    mask: last is max(i + 1, the end of the prefix); padding: first = last."""
+
+    def __init__(self, cap: float = 0.0, slopes: torch.Tensor | None = None,
+                 first: torch.Tensor | None = None, last: torch.Tensor | None = None,
+                 causal: bool = True):
+        self.cap, self.slopes, self.first, self.last, self.causal = cap, slopes, first, last, causal
+        self.desc = KLScoring(cap, _ptr(slopes), _ptr(first), _ptr(last), int(causal))
+
+    def checked(self, B: int, N: int, H: int, dev: int):
+        """The descriptor, once its tensors fit a call on [B, N, H, d] tensors."""
+        _like(self.slopes, (H,), torch.float32, dev, "slopes")
+        _like(self.first, (B, N), torch.int32, dev, "first")
+        _like(self.last, (B, N), torch.int32, dev, "last")
+        return ctypes.byref(self.desc)
+
+
+def keyless_scored_forward(q_routed: torch.Tensor, v: torch.Tensor, scoring: Scoring,
+                           scale: float = 0.0, out=None, lse=None, out_f32=None):
+    """keyless_attention_forward with the scores and masks of ``scoring``; returns (out, lse)."""
+    load()
+    B, N, H, dk = q_routed.shape
+    G, dev, dt = v.shape[2], q_routed.get_device(), q_routed.dtype
+    if out is None:
+        out = torch.empty_like(q_routed)
+    if lse is None:
+        lse = torch.empty((B, H, N), dtype=torch.float32, device=q_routed.device)
+    _call(dev, _lib.keyless_scored_forward, _ptr(q_routed), _like(v, (B, N, G, dk), dt, dev, "v"),
+          scoring.checked(B, N, H, dev), B, N, H, G, dk, scale, _dt(q_routed),
+          _like(out, (B, N, H, dk), dt, dev, "out"), _like(lse, (B, H, N), torch.float32, dev, "lse"),
+          _like(out_f32, (B, N, H, dk), torch.float32, dev, "out_f32"))
+    return out, lse
+
+
+def scored_backward_workspace_bytes(B: int, N: int, H: int, G: int, d_head: int,
+                                    dtype: torch.dtype) -> int:
+    load()
+    return int(_lib.keyless_scored_backward_workspace_size(
+        B, N, H, G, d_head, KL_BF16 if dtype == torch.bfloat16 else KL_F32))
+
+
+def keyless_scored_backward(q_routed: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                            dout: torch.Tensor, lse: torch.Tensor, scoring: Scoring,
+                            scale: float = 0.0, dq=None, dv=None, workspace=None, out_f32=None):
+    """(dq_routed, dv) of keyless_scored_forward from dout and what that call returned
+    (and its fp32 output, when kept)."""
+    load()
+    B, N, H, dk = q_routed.shape
+    G, dev, dt = v.shape[2], q_routed.get_device(), q_routed.dtype
+    if dq is None:
+        dq = torch.empty_like(q_routed)
+    if dv is None:
+        dv = torch.empty_like(v)
+    if workspace is None:
+        n = scored_backward_workspace_bytes(B, N, H, G, dk, dt)
+        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=q_routed.device)
+    like_q = (B, N, H, dk)
+    _call(dev, _lib.keyless_scored_backward, _ptr(q_routed), _like(v, (B, N, G, dk), dt, dev, "v"),
+          _like(out, like_q, dt, dev, "out"), _like(out_f32, like_q, torch.float32, dev, "out_f32"),
+          _like(dout, like_q, dt, dev, "dout"), _like(lse, (B, H, N), torch.float32, dev, "lse"),
+          scoring.checked(B, N, H, dev), B, N, H, G, dk, scale, _dt(q_routed),
+          _like(dq, like_q, dt, dev, "dq"), _like(dv, (B, N, G, dk), dt, dev, "dv"), _ptr(workspace),
+          workspace.numel() * workspace.element_size())
+    return dq, dv
+
+
+def tree_decode_workspace_bytes(cache: ValueCache, B: int, T: int, H: int) -> int:
+    load()
+    return int(_lib.keyless_tree_decode_workspace_size(cache.ref, B, T, H))
+
+
+def _per_sequence(cache: ValueCache, t: torch.Tensor, B: int, dev: int, what: str):
+    rows = cache.block_table if cache.block_table is not None else cache.data
+    if rows.shape[0] != B:
+        raise ValueError(f"the cache holds {rows.shape[0]} sequences, not {B}")
+    return _like(t, (B,), torch.int32, dev, what)
+
+
+def keyless_tree_decode(q_routed: torch.Tensor, cache: ValueCache, lengths_before: torch.Tensor,
+                        tree: torch.Tensor | None = None, cap: float = 0.0,
+                        slopes: torch.Tensor | None = None, scale: float = 0.0, out=None,
+                        workspace=None) -> torch.Tensor:
+    """T drafted tokens per sequence, q~ [B, T, H, d], over the rows cached before them and
+    the drafted rows that ``tree`` lets each see (int64 [B, T], bit u of word t: token t sees
+    drafted row u, at position lengths_before[b] + u of the cache; None: a chain)."""
+    load()
+    B, T, H, dk = q_routed.shape
+    dev = q_routed.get_device()
+    if dk != cache.desc.d_head or q_routed.dtype != cache.data.dtype:
+        raise ValueError("q_routed and the cache differ in d_head or dtype")
+    if out is None:
+        out = torch.empty_like(q_routed)
+    if workspace is None:
+        n = tree_decode_workspace_bytes(cache, B, T, H)
+        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=q_routed.device)
+    _call(dev, _lib.keyless_tree_decode, _ptr(q_routed), cache.ref,
+          _per_sequence(cache, lengths_before, B, dev, "lengths_before"),
+          _like(tree, (B, T), torch.int64, dev, "tree"), B, T, H, cap,
+          _like(slopes, (H,), torch.float32, dev, "slopes"), scale,
+          _like(out, q_routed.shape, q_routed.dtype, dev, "out"), _ptr(workspace),
+          workspace.numel() * workspace.element_size())
+    return out
+
+
+def value_cache_keep(cache: ValueCache, lengths_before: torch.Tensor, path: torch.Tensor,
+                     kept: torch.Tensor):
+    """The accepted drafted rows move up: row lengths_before[b] + k becomes row
+    lengths_before[b] + path[b, k] for k < kept[b] (path int32 [B, T])."""
+    load()
+    B, T = path.shape
+    dev = cache.data.get_device()
+    _call(dev, _lib.value_cache_keep, cache.ref,
+          _per_sequence(cache, lengths_before, B, dev, "lengths_before"),
+          _like(path, (B, T), torch.int32, dev, "path"), _like(kept, (B,), torch.int32, dev, "kept"),
+          B, T)

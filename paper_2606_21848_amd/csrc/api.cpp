@@ -1262,4 +1262,191 @@ int keyless_weight_gradients(const void* x, const void* W_Q, const void* W_R, co
   return s;
 }
 
+namespace {
+
+int check_scored_args(const char* who, const void* q, const void* v, const void* out,
+                      const kl_scoring* sc, int B, int N, int H, int G, int d_head, kl_dtype dtype,
+                      float scale) {
+  int s = check_prefill_args(who, q, v, out, B, N, 64, H, G, d_head, dtype, scale);
+  if (s != KL_OK) return s;
+  if (!sc) return fail(KL_ERR_INVALID_ARG, "%s: scoring is NULL", who);
+  if (!(sc->cap >= 0.f) || std::isinf(sc->cap))
+    return fail(KL_ERR_INVALID_ARG, "%s: cap must be finite and >= 0 (0 = none)", who);
+  if (std::isinf(scale)) return fail(KL_ERR_INVALID_ARG, "%s: scale must be finite", who);
+  // Rows of a sequence are addressed with 32-bit byte offsets inside a tile, and the
+  // grid holds one workgroup per head and 16 rows at most.
+  if ((long)H * d_head >= (1L << 24))
+    return fail(KL_ERR_UNSUPPORTED, "%s: rows of H * d_head elements must be shorter than 2^24", who);
+  if ((double)B * H * ((N + 15) / 16) >= 2147483648.0)
+    return fail(KL_ERR_UNSUPPORTED, "%s: B * H * N too large", who);
+  return KL_OK;
+}
+
+kl::ScoredParams scored_params(const void* q, const void* v, const kl_scoring* sc, int B, int N,
+                               int H, int G, int d_head, float scale, kl_dtype dtype) {
+  kl::ScoredParams p{};
+  p.q = q;
+  p.v = v;
+  p.slopes = sc->slopes;
+  p.first = sc->first;
+  p.last = sc->last;
+  p.causal = sc->causal ? 1 : 0;
+  p.B = B;
+  p.N = N;
+  p.H = H;
+  p.G = G;
+  p.D = d_head;
+  p.scale = scale_or_default(scale, d_head);
+  p.cap = sc->cap;
+  p.dtype = dtype;
+  return p;
+}
+
+}  // namespace
+
+int keyless_scored_forward(const void* q_routed, const void* v, const kl_scoring* scoring, int B,
+                           int N, int H, int G, int d_head, float scale, kl_dtype dtype, void* out,
+                           float* lse, float* out_f32, void* stream) {
+  const char* who = "keyless_scored_forward";
+  int s = check_scored_args(who, q_routed, v, out, scoring, B, N, H, G, d_head, dtype, scale);
+  if (s != KL_OK) return s;
+  if (!aligned16(q_routed) || !aligned16(v) || !aligned16(out) || !aligned16(out_f32))
+    return fail(KL_ERR_INVALID_ARG, "%s: q_routed, v, out and out_f32 must be 16-byte aligned", who);
+  if (B == 0 || N == 0) return KL_OK;
+  kl::ScoredParams p = scored_params(q_routed, v, scoring, B, N, H, G, d_head, scale, dtype);
+  p.out = out;
+  p.lse = lse;
+  p.out_f32 = out_f32;
+  return hip_status(kl::launch_scored_forward(p, static_cast<hipStream_t>(stream)), who);
+}
+
+size_t keyless_scored_backward_workspace_size(int B, int N, int H, int G, int d_head,
+                                              kl_dtype dtype) {
+  if (B < 0 || N < 0 || H <= 0 || G <= 0 || H % G != 0 || d_head <= 0 || !dtype_ok(dtype)) return 0;
+  return bwd_rows_bytes(B, N, H);
+}
+
+int keyless_scored_backward(const void* q_routed, const void* v, const void* out,
+                            const float* out_f32, const void* dout, const float* lse,
+                            const kl_scoring* scoring, int B, int N, int H, int G, int d_head,
+                            float scale, kl_dtype dtype, void* dq_routed, void* dv, void* ws,
+                            size_t ws_bytes, void* stream) {
+  const char* who = "keyless_scored_backward";
+  int s = check_scored_args(who, q_routed, v, out, scoring, B, N, H, G, d_head, dtype, scale);
+  if (s != KL_OK) return s;
+  if (!dout || !lse || !dq_routed || !dv)
+    return fail(KL_ERR_INVALID_ARG, "%s: dout, lse, dq_routed and dv must be non-NULL", who);
+  for (const void* t : {q_routed, v, out, static_cast<const void*>(out_f32), dout,
+                        static_cast<const void*>(dq_routed), static_cast<const void*>(dv)})
+    if (!aligned16(t)) return fail(KL_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
+  const size_t need = keyless_scored_backward_workspace_size(B, N, H, G, d_head, dtype);
+  if (need && (!ws || ws_bytes < need))
+    return fail(KL_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need, ws_bytes);
+  if (!aligned16(ws)) return fail(KL_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
+  if (B == 0 || N == 0) return KL_OK;
+  kl::ScoredParams p = scored_params(q_routed, v, scoring, B, N, H, G, d_head, scale, dtype);
+  p.lse = const_cast<float*>(lse);
+  p.out_f32 = const_cast<float*>(out_f32);
+  p.out_in = out;
+  p.dout = dout;
+  p.Dd = static_cast<float*>(ws);
+  p.dq = dq_routed;
+  p.dv = dv;
+  return hip_status(kl::launch_scored_backward(p, static_cast<hipStream_t>(stream)), who);
+}
+
+size_t keyless_tree_decode_workspace_size(const kl_value_cache* cache, int B, int T, int H) {
+  if (!cache || B <= 0 || T <= 0 || T > kl::kMaxDrafts || H <= 0 || cache->G <= 0 || H % cache->G != 0)
+    return 0;
+  return 0;
+}
+
+int keyless_tree_decode(const void* q_routed, const kl_value_cache* cache,
+                        const int32_t* lengths_before, const uint64_t* tree, int B, int T, int H,
+                        float cap, const float* slopes, float scale, void* out, void* ws,
+                        size_t ws_bytes, void* stream) {
+  const char* who = "keyless_tree_decode";
+  int s = check_cache(cache, who);
+  if (s != KL_OK) return s;
+  if (!q_routed || !lengths_before || !out)
+    return fail(KL_ERR_INVALID_ARG, "%s: q_routed, lengths_before and out must be non-NULL", who);
+  if (!aligned16(q_routed) || !aligned16(out))
+    return fail(KL_ERR_INVALID_ARG, "%s: q_routed and out must be 16-byte aligned", who);
+  if (reinterpret_cast<uintptr_t>(tree) & 7u)
+    return fail(KL_ERR_INVALID_ARG, "%s: tree must be 8-byte aligned", who);
+  if (B < 0 || H <= 0) return fail(KL_ERR_INVALID_ARG, "%s: bad B=%d or H=%d", who, B, H);
+  if (T < 1 || T > kl::kMaxDrafts)
+    return fail(KL_ERR_UNSUPPORTED, "%s: T=%d drafted tokens (1 to %d)", who, T, kl::kMaxDrafts);
+  if (H % cache->G != 0)
+    return fail(KL_ERR_INVALID_ARG, "%s: H=%d is not a multiple of G=%d", who, H, cache->G);
+  if (!(cap >= 0.f) || std::isinf(cap))
+    return fail(KL_ERR_INVALID_ARG, "%s: cap must be finite and >= 0 (0 = none)", who);
+  if (!(scale >= 0.f) || std::isinf(scale))
+    return fail(KL_ERR_INVALID_ARG, "%s: scale must be finite and >= 0 (0 = 1/sqrt(d_head))", who);
+  if (cache_capacity(cache) > (1 << 30))
+    return fail(KL_ERR_UNSUPPORTED, "%s: capacity per sequence too large", who);
+  if ((double)B * H * T >= 2147483648.0)
+    return fail(KL_ERR_UNSUPPORTED, "%s: B * H * T too large", who);
+  if (B == 0) return KL_OK;
+  const size_t need = keyless_tree_decode_workspace_size(cache, B, T, H);
+  if (need && (!ws || ws_bytes < need))
+    return fail(KL_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need, ws_bytes);
+  if (need && !aligned16(ws))
+    return fail(KL_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
+  kl::TreeParams p{};
+  p.q = q_routed;
+  p.data = cache->data;
+  p.table = cache->layout == KL_PAGED ? cache->block_table : nullptr;
+  p.lengths = lengths_before;
+  p.tree = tree;
+  p.slopes = slopes;
+  p.out = out;
+  p.B = B;
+  p.T = T;
+  p.H = H;
+  p.G = cache->G;
+  p.D = cache->d_head;
+  p.dtype = cache->dtype;
+  p.paged = cache->layout == KL_PAGED;
+  p.L_max = cache->L_max;
+  p.block_shift = p.paged ? log2_exact(cache->block_size) : 0;
+  p.num_blocks = cache->num_blocks;
+  p.max_blocks = cache->max_blocks_per_seq;
+  p.scale = scale_or_default(scale, p.D);
+  p.cap = cap;
+  return hip_status(kl::launch_tree_decode(p, static_cast<hipStream_t>(stream)), who);
+}
+
+int value_cache_keep(const kl_value_cache* cache, const int32_t* lengths_before,
+                     const int32_t* path, const int32_t* kept, int B, int T, void* stream) {
+  const char* who = "value_cache_keep";
+  int s = check_cache(cache, who);
+  if (s != KL_OK) return s;
+  if (!lengths_before || !path || !kept)
+    return fail(KL_ERR_INVALID_ARG, "%s: lengths_before, path and kept must be non-NULL", who);
+  if (B < 0 || T < 0) return fail(KL_ERR_INVALID_ARG, "%s: bad B=%d or T=%d", who, B, T);
+  if (T > kl::kMaxDrafts)
+    return fail(KL_ERR_UNSUPPORTED, "%s: T=%d drafted tokens (at most %d)", who, T, kl::kMaxDrafts);
+  if ((double)B * cache->G >= 2147483648.0)
+    return fail(KL_ERR_UNSUPPORTED, "%s: B * G too large", who);
+  if (B == 0 || T == 0) return KL_OK;
+  kl::KeepParams p{};
+  p.data = cache->data;
+  p.table = cache->layout == KL_PAGED ? cache->block_table : nullptr;
+  p.lengths_before = lengths_before;
+  p.path = path;
+  p.kept = kept;
+  p.B = B;
+  p.T = T;
+  p.G = cache->G;
+  p.D = cache->d_head;
+  p.dtype = cache->dtype;
+  p.paged = cache->layout == KL_PAGED;
+  p.L_max = cache->L_max;
+  p.block_shift = p.paged ? log2_exact(cache->block_size) : 0;
+  p.num_blocks = cache->num_blocks;
+  p.max_blocks = cache->max_blocks_per_seq;
+  return hip_status(kl::launch_keep(p, static_cast<hipStream_t>(stream)), who);
+}
+
 }  // extern "C"

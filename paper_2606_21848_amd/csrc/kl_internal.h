@@ -258,6 +258,66 @@ hipError_t launch_attention_backward_f32(const BwdParams& p, hipStream_t stream)
 // VALU attention for what the kernels above do not take.
 hipError_t launch_prefill_attention_simple(const AttnParams& p, hipStream_t stream);
 
+// Scored attention (a tanh cap, a distance bias, a range of seen rows per query)
+// over q, dout, out, dq [B, N, H, D] and v, dv [B, N, G, D], contiguous.
+struct ScoredParams {
+  const void* q;
+  const void* v;
+  void* out;             // forward
+  float* lse;            // [B, H, N]: written by the forward (may be null), read by the backward
+  float* out_f32;        // [B, N, H, D] or null
+  const float* slopes;   // [H] or null
+  const int32_t* first;  // [B, N] or null: the first row a query sees
+  const int32_t* last;   // [B, N] or null: the row after the last one it sees
+  int causal;            // with last == null: i + 1, else N
+  int B, N, H, G, D;
+  float scale, cap;      // cap 0 for none
+  kl_dtype dtype;
+  // Backward.
+  const void* dout;
+  const void* out_in;    // the forward's output
+  float* Dd;             // [B, H, N] scratch: rowsum(P * dP)
+  void* dq;
+  void* dv;
+};
+hipError_t launch_scored_forward(const ScoredParams& p, hipStream_t stream);
+hipError_t launch_scored_backward(const ScoredParams& p, hipStream_t stream);
+
+// Most drafted tokens per sequence: a token's row of the tree is one 64-bit word.
+constexpr int kMaxDrafts = 64;
+
+// Attention of T drafted tokens per sequence (q, out [B, T, H, D]) over the cached
+// rows and the drafted rows that follow them.
+struct TreeParams {
+  const void* q;
+  const void* data;
+  const int32_t* table;
+  const int32_t* lengths;  // [B] rows before the draft
+  const uint64_t* tree;    // [B, T] or null (a chain)
+  const float* slopes;     // [H] or null
+  void* out;
+  int B, T, H, G, D;
+  kl_dtype dtype;
+  bool paged;
+  int L_max, block_shift, num_blocks, max_blocks;
+  float scale, cap;
+};
+hipError_t launch_tree_decode(const TreeParams& p, hipStream_t stream);
+
+// Rows n + path[b, k] to rows n + k for k < kept[b], n = lengths_before[b].
+struct KeepParams {
+  void* data;
+  const int32_t* table;
+  const int32_t* lengths_before;
+  const int32_t* path;  // [B, T]
+  const int32_t* kept;  // [B]
+  int B, T, G, D;
+  kl_dtype dtype;
+  bool paged;
+  int L_max, block_shift, num_blocks, max_blocks;
+};
+hipError_t launch_keep(const KeepParams& p, hipStream_t stream);
+
 // Measuring kernels (not part of the method): a streaming read of bytes (a
 // multiple of 16, src 16-byte aligned) and a loop of matrix-core products,
 // 4 waves x iters x 16 products of 16 x 16 x 32 per workgroup.

@@ -1,0 +1,327 @@
+"""Drafted tokens over a value-only cache (trees and chains, cap and bias, contiguous
+and paged) and the keeping of accepted rows, against the 64-bit oracle."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import scored as S
+from oracle.keyless import cache_rows, default_scale
+from paper_2606_21848_amd import binding as kb
+from tests.parity import say, to64
+from tests.scored_tol import E, check
+from tests.test_gpu_scored import gpu, slopes_of
+from workloads import synth
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+TYPES = [torch.float32, torch.bfloat16]
+SCORES = [(0.0, False), (4.0, True), (20.0, False)]
+
+
+def make_cache(dtype, B, G, d, room, layout, seed, bs=16):
+    """(ValueCache, its host copy, host table, room): block ids in no order."""
+    if layout == "contiguous":
+        c = synth.normal((B, G, room, d), seed, 1, 1.0, dtype)
+        return kb.ValueCache(c.to(DEV)), c, None, room
+    width = -(-room // bs)
+    c = synth.normal((B * width + 3, G, bs, d), seed, 1, 1.0, dtype)
+    table = np.random.RandomState(seed).permutation(B * width + 3)[:B * width].reshape(B, width)
+    return kb.ValueCache(c.to(DEV), gpu(table, torch.int32)), c, table, width * bs
+
+
+def random_tree(B, T, seed):
+    rs = np.random.RandomState(seed)
+    parents = [[-1] + [rs.randint(-1 if t % 5 == 4 else 0, t) for t in range(1, T)] for _ in range(B)]
+    return S.tree_words(parents)
+
+
+def tree_bound(q, cache, n, tree, H, G, cap, sl, table, bs, bf16, capacity):
+    """As scored_tol.bounds, for the output of a draft."""
+    ref = S.tree_decode(q, cache, n, tree, H, G, cap, sl, table, bs, None, capacity)
+    u = 2.0 ** -8 if bf16 else E
+    B, T, _, d = q.shape
+    tol = np.zeros(q.shape)
+    for b in range(B):
+        rows = min(int(n[b]) + T, capacity)
+        words = [(2 << t) - 1 if tree is None else int(tree[b][t]) & ((1 << T) - 1) for t in range(T)]
+        sees = np.array([[bool(w >> k & 1) for k in range(T)] for w in words])
+        depth = sees.sum(1) - np.diag(sees)
+        pos = np.concatenate([np.arange(int(n[b])), int(n[b]) + depth])[:rows]
+        seen = np.concatenate([np.ones((T, int(n[b])), bool), sees], 1)[:, :rows]
+        dist = np.abs((int(n[b]) + depth)[:, None] - pos[None])
+        for h in range(H):
+            V = cache_rows(cache, b, h // (H // G), rows, table, bs)
+            slope = 0.0 if sl is None else sl[h]
+            x, _ = S.scores(q[b, :, h], V, default_scale(d), cap, slope, dist)
+            P, lse = S.masked_softmax(x, seen)
+            lse = np.where(np.isinf(lse), 0.0, lse)
+            sizes = default_scale(d) * (np.abs(q[b, :, h]) @ np.abs(V).T)
+            dl = E * ((2 * d + 8) * sizes + 8 * (np.abs(x) + abs(slope) * dist + np.abs(lse)[:, None])) \
+                + 2.0 ** -21 * cap
+            dl = np.max(np.where(seen, dl, 0.0), axis=1, initial=0.0)[:, None]
+            tol[b, :, h] = u * np.abs(ref[b, :, h]) + ((u if bf16 else 0.0) + 2 * dl + 2.0 ** -20 + rows * E) \
+                * (P @ np.abs(V))
+    return ref, tol
+
+
+# Heads per group 1, 2, 3, 6, 8 and 40; T of one, odd, a whole word; lengths of zero and
+# one, ends of pages and tiles, and a draft that runs past the capacity.
+SHAPES = [(1, 1, 12, 2, 128, [300]), (3, 5, 4, 4, 64, [0, 1, 130]), (2, 7, 6, 2, 128, [16, 255]),
+          (4, 64, 3, 1, 128, [0, 31, 64, 97]), (2, 16, 16, 2, 64, [500, 33]), (1, 3, 40, 1, 128, [77]),
+          (5, 2, 8, 8, 128, [1, 0, 15, 1000, 47])]
+
+
+@pytest.mark.parametrize("layout", ["contiguous", "paged"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,T,H,G,d,n", SHAPES)
+def test_tree_matches_oracle(lib, dtype, layout, B, T, H, G, d, n):
+    vc, c, table, room = make_cache(dtype, B, G, d, max(n) + T + 5, layout, 401)
+    q = synth.normal((B, T, H, d), 401, 2, 3.0, dtype)
+    words = random_tree(B, T, 402)
+    words[-1, T // 2] = 0  # a drafted token that sees the cached rows alone
+    for cap, bias in SCORES:
+        for tree in (None, words):
+            say(f"tree {dtype} {layout} B={B} T={T} H={H} G={G} d={d} n={n} cap={cap} bias={bias} "
+                f"chain={tree is None}")
+            sl = slopes_of(H) if bias else None
+            got = kb.keyless_tree_decode(q.to(DEV), vc, gpu(n, torch.int32), cap=cap, slopes=gpu(sl),
+                                         tree=None if tree is None else gpu(tree.view(np.int64)))
+            torch.cuda.synchronize()
+            ref, tol = tree_bound(to64(q), to64(c), n, tree, H, G, cap, sl, table, 16,
+                                  dtype == torch.bfloat16, room)
+            check("tree", to64(got), ref, tol)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,n,L", [(1, 9000, 9001), (24, 6000, 6100), (64, 20000, 20064)])
+def test_long_caches(lib, dtype, T, n, L):
+    """Caches long enough to be split, beside a short and an empty one in the batch."""
+    B, H, G, d = 3, 8, 4, 128
+    say(f"tree, long caches T={T} n={n} {dtype}")
+    lens = [n, 40, 0]
+    c = synth.normal((B, G, L, d), 403, 1, 1.0, dtype)
+    q = synth.normal((B, T, H, d), 403, 2, 1.0, dtype)
+    words = random_tree(B, T, 404)
+    sl = slopes_of(H) * 0.01
+    vc = kb.ValueCache(c.to(DEV))
+    got = kb.keyless_tree_decode(q.to(DEV), vc, gpu(lens, torch.int32), gpu(words.view(np.int64)),
+                                 cap=30.0, slopes=gpu(sl))
+    again = kb.keyless_tree_decode(q.to(DEV), vc, gpu(lens, torch.int32), gpu(words.view(np.int64)),
+                                   cap=30.0, slopes=gpu(sl))
+    torch.cuda.synchronize()
+    assert torch.equal(got, again)
+    ref, tol = tree_bound(to64(q), to64(c), lens, words, H, G, 30.0, sl, None, 16,
+                          dtype == torch.bfloat16, L)
+    check("tree", to64(got), ref, tol)
+
+
+def test_offsets_past_32_bits(lib):
+    """A cache of more than 4 GiB, the rows read at its far end."""
+    B, T, H, G, d, L = 3, 2, 2, 2, 128, 4 << 20
+    say("tree, 4 GiB and more")
+    data = torch.zeros((B, G, L, d), dtype=torch.bfloat16, device=DEV)  # 6.4 GB
+    rows = synth.normal((G, 64, d), 405, 1, 1.0, torch.bfloat16)
+    data[2, :, :64] = rows.to(DEV)
+    q = synth.normal((B, T, H, d), 405, 2, 2.0, torch.bfloat16)
+    n = [0, 1, 62]
+    got = kb.keyless_tree_decode(q.to(DEV), kb.ValueCache(data), gpu(n, torch.int32))
+    path, kept = gpu([[0, 1], [0, 1], [1, 1]], torch.int32), gpu([0, 0, 2], torch.int32)
+    kb.value_cache_keep(kb.ValueCache(data), gpu(n, torch.int32), path, kept)
+    torch.cuda.synchronize()
+    small = np.zeros((B, G, 64, d))
+    small[2] = to64(rows)
+    ref, tol = tree_bound(to64(q), small, n, None, H, G, 0.0, None, None, 16, True, 64)
+    check("tree", to64(got), ref, tol)
+    assert torch.equal(data[2, :, 62], rows[:, 63].to(DEV)) and torch.equal(data[2, :, 63], rows[:, 63].to(DEV))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_rows_not_seen_never_matter(lib, dtype, bad):
+    """Rows past the draft, blocks that no sequence owns, drafted rows of other branches
+    (NaN or infinite): nothing of them reaches a token that does not see them."""
+    B, T, H, G, d = 2, 6, 4, 2, 128
+    say(f"tree, {bad} in rows not seen, {dtype}")
+    vc, c, table, room = make_cache(dtype, B, G, d, 90, "paged", 406)
+    n = [37, 70]
+    words = S.tree_words([[-1, 0, 0, 1, 2, 2]] * B)
+    q = synth.normal((B, T, H, d), 406, 2, 3.0, dtype).to(DEV)
+    args = (q, vc, gpu(n, torch.int32), gpu(words.view(np.int64)))
+    for cap in (0.0, 20.0):
+        clean = kb.keyless_tree_decode(*args, cap=cap)
+        torch.cuda.synchronize()
+        data = vc.data.clone()
+        owned = set(table.reshape(-1).tolist())
+        for blk in range(c.shape[0]):
+            if blk not in owned:
+                vc.data[blk] = bad
+        for b in range(B):
+            for pos in list(range(n[b] + T, room)) + [n[b] + 2]:  # past the draft, and token 2
+                vc.data[int(table[b][pos // 16]), :, pos % 16, 5:9] = bad
+        got = kb.keyless_tree_decode(*args, cap=cap)
+        torch.cuda.synchronize()
+        for t in (0, 1, 3):
+            assert torch.equal(got[:, t], clean[:, t])
+        for t in (2, 4, 5):
+            assert not torch.isfinite(got[:, t, :, 5:9]).any()
+        vc.data.copy_(data)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_bad_lengths_tables_and_words(lib, dtype):
+    """Lengths out of range are clamped, blocks outside the cache are empty, bits past T
+    are not read, a draft at the end of the capacity loses its last rows."""
+    B, T, H, G, d = 3, 4, 2, 1, 64
+    say(f"tree, bad device data, {dtype}")
+    vc, c, table, room = make_cache(dtype, B, G, d, 64, "paged", 407)
+    table = table.copy()
+    q = synth.normal((B, T, H, d), 407, 2, 1.0, dtype)
+    bad = table.copy()
+    bad[1, 1], bad[1, 2] = -1, c.shape[0]
+    lens = [-5, 60, 2 ** 31 - 1]
+    words = random_tree(B, T, 408)
+    got = kb.keyless_tree_decode(q.to(DEV), kb.ValueCache(vc.data, gpu(bad, torch.int32)),
+                                 gpu(lens, torch.int32), gpu((words | np.uint64(0xFFFF << 8)).view(np.int64)))
+    torch.cuda.synchronize()
+    # Sequence 1 without its rows 16 .. 47 (a cache of its other rows).
+    ref = np.zeros((B, T, H, d))
+    ref[0] = S.tree_decode(to64(q)[:1], to64(c), [0], words[:1], H, G, 0.0, None, table[:1], 16)[0]
+    ref[2] = S.tree_decode(to64(q)[2:], to64(c), [room], words[2:], H, G, 0.0, None, table[2:], 16, None, room)[0]
+    rows = np.concatenate([cache_rows(to64(c), 1, 0, 16, table), cache_rows(to64(c), 1, 0, 64, table)[48:]])
+    ref[1] = S.tree_decode(to64(q)[1:2], rows[None, None], [28], words[1:2], H, G)[0]
+    tol = 3e-2 if dtype == torch.bfloat16 else 1e-4
+    assert np.abs(to64(got) - ref).max() <= tol
+
+
+@pytest.mark.parametrize("layout", ["contiguous", "paged"])
+@pytest.mark.parametrize("dtype,G,d", [(torch.bfloat16, 2, 128), (torch.bfloat16, 3, 64), (torch.float32, 2, 128),
+                                       (torch.float32, 1, 64)])
+def test_keep_moves_rows_bit_for_bit(lib, dtype, G, d, layout):
+    """Paths that rise, fall, repeat a row and leave the range; kept counts of none, all
+    and out of range; lengths at the end of the capacity."""
+    B, T = 7, 64
+    say(f"keep {dtype} {layout} G={G} d={d}")
+    vc, c, table, room = make_cache(dtype, B, G, d, 200, layout, 409)
+    rs = np.random.RandomState(410)
+    n = np.array([0, 1, 100, 130, room - 64, 16, 90])
+    kept = np.array([64, 0, 13, 30, 64, 5, 64])
+    path = np.stack([np.sort(rs.permutation(T)) if b % 2 else rs.randint(0, T, T) for b in range(B)])
+    path[2, :13] = np.arange(13) * 4
+    path[5, :5] = 7
+    kb.value_cache_keep(vc, gpu(n, torch.int32), gpu(path, torch.int32), gpu(kept, torch.int32))
+    torch.cuda.synchronize()
+    ref = S.value_cache_keep(c.view(torch.int16).numpy() if dtype == torch.bfloat16 else c.numpy(), n, path, kept,
+                             table)
+    got = vc.data.cpu()
+    assert np.array_equal(got.view(torch.int16).numpy() if dtype == torch.bfloat16 else got.numpy(), ref)
+    # Entries outside [0, T), rows past the capacity, negative counts: nothing moves.
+    before = vc.data.clone()
+    path[:] = [-1, T, 2 ** 31 - 1, -(2 ** 31)] * (T // 4)
+    kb.value_cache_keep(vc, gpu(n, torch.int32), gpu(path, torch.int32), gpu(kept, torch.int32))
+    kb.value_cache_keep(vc, gpu(n * 0 + room, torch.int32), gpu(path * 0, torch.int32), gpu(kept, torch.int32))
+    kb.value_cache_keep(vc, gpu(n * 0 + 2 ** 31 - 1, torch.int32), gpu(path * 0 + 3, torch.int32), gpu(kept, torch.int32))
+    kb.value_cache_keep(vc, gpu(n, torch.int32), gpu(path * 0 + 1, torch.int32), gpu(-kept, torch.int32))
+    torch.cuda.synchronize()
+    assert torch.equal(vc.data, before)
+
+
+@pytest.mark.parametrize("layout", ["contiguous", "paged"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_draft_step(lib, dtype, layout):
+    """The calls of speculative serving in order: the draft's values are appended, the
+    tree attends, a path is kept, and the next token decodes over it; the same as
+    appending the accepted tokens alone."""
+    B, T, H, G, d = 3, 6, 4, 2, 128
+    say(f"draft step {dtype} {layout}")
+    vc, c, table, room = make_cache(dtype, B, G, d, 60, layout, 411)
+    n = gpu([33, 0, 14], torch.int32)
+    drafted = synth.normal((B, T, G, d), 411, 3, 1.0, dtype).to(DEV)
+    words = S.tree_words([[-1, 0, 0, 1, 2, 4]] * B)
+    q = synth.normal((B, T, H, d), 411, 4, 2.0, dtype).to(DEV)
+    plain = kb.ValueCache(vc.data.clone(), vc.block_table)
+    kb.value_cache_append(vc, drafted, n)
+    out = kb.keyless_tree_decode(q, vc, n, gpu(words.view(np.int64)))
+    path = gpu([[0, 2, 4, 5, 0, 0], [0, 1, 3, 0, 0, 0], [0, 0, 0, 0, 0, 0]], torch.int32)
+    kept = gpu([4, 3, 1], torch.int32)
+    kb.value_cache_keep(vc, n, path, kept)
+    # The accepted tokens alone: token by token with the decode that the framework has.
+    k = [4, 3, 1]
+    for step in range(4):
+        at = path[:, min(step, 3)].long()
+        rows, heads = drafted[torch.arange(B), at][:, None].contiguous(), q[torch.arange(B), at].contiguous()
+        before = n + torch.tensor([min(step, x - 1) for x in k], dtype=torch.int32, device=DEV)
+        kb.value_cache_append(plain, rows, before)
+        one = kb.keyless_decode(heads, plain, before + 1)
+        torch.cuda.synchronize()
+        for b in range(B):
+            if step < k[b]:
+                err = (out[b, at[b]].float() - one[b].float()).abs().max()
+                assert err <= (2e-2 if dtype == torch.bfloat16 else 1e-4) * one[b].float().abs().max()
+        if step >= 1:  # sequences that are done append their last row again, at its place
+            path = torch.where(torch.arange(T, device=DEV)[None] < kept[:, None], path, path.gather(
+                1, (kept[:, None] - 1).long().expand(B, T)))
+    nxt = synth.normal((B, H, d), 411, 5, 1.0, dtype).to(DEV)
+    a = kb.keyless_decode(nxt, vc, n + kept)
+    whole = kb.keyless_tree_decode(nxt[:, None].contiguous(), vc, n + kept - 1)
+    torch.cuda.synchronize()
+    for b in range(B):
+        for g in range(G):
+            rows = int(n[b]) + k[b]
+            x = cache_rows(to64(vc.data), b, g, rows, table)
+            y = cache_rows(to64(plain.data), b, g, rows, table)
+            assert np.array_equal(x, y), (b, g)
+    assert (whole[:, 0].float() - a.float()).abs().max() <= (2e-2 if dtype == torch.bfloat16 else 1e-5) * 3
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_draft_step_graph_replays(lib, dtype):
+    """Append, tree attention and keep captured once, replayed with eager work between;
+    two captured graphs have workspaces of their own."""
+    B, T, H, G, d, L = 3, 8, 8, 2, 128, 3000
+    say(f"tree graph {dtype}")
+    n = gpu([2900, 10, 1500], torch.int32)
+    words = gpu(random_tree(B, T, 412).view(np.int64))
+    path, kept = gpu([[0, 2, 5, 7, 0, 0, 0, 0]] * B, torch.int32), gpu([4, 2, 0], torch.int32)
+    sl = gpu(slopes_of(H))
+    base = synth.normal((B, G, L, d), 412, 1, 1.0, dtype).to(DEV)
+    q, rows = torch.empty((B, T, H, d), dtype=dtype, device=DEV), torch.empty((B, T, G, d), dtype=dtype, device=DEV)
+    graphs = []
+    for _ in range(2):
+        vc = kb.ValueCache(base.clone())
+        out = torch.empty_like(q)
+        ws = torch.full((max(256, kb.tree_decode_workspace_bytes(vc, B, T, H)),), 0xFF, dtype=torch.uint8, device=DEV)
+
+        def step(vc=vc, out=out, ws=ws):
+            kb.value_cache_append(vc, rows, n)
+            kb.keyless_tree_decode(q, vc, n, words, cap=25.0, slopes=sl, out=out, workspace=ws)
+            kb.value_cache_keep(vc, n, path, kept)
+        q.copy_(synth.normal((B, T, H, d), 413, 1, 1.0, dtype))
+        rows.copy_(synth.normal((B, T, G, d), 413, 2, 1.0, dtype))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step()
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step()
+        graphs.append((g, vc, out))
+    for rep in range(3):
+        q.copy_(synth.normal((B, T, H, d), 420 + rep, 1, 1.0, dtype))
+        rows.copy_(synth.normal((B, T, G, d), 420 + rep, 2, 1.0, dtype))
+        ref = kb.ValueCache(base.clone())
+        kb.value_cache_append(ref, rows, n)
+        want = kb.keyless_tree_decode(q, ref, n, words, cap=25.0, slopes=sl)
+        kb.value_cache_keep(ref, n, path, kept)
+        for _, vc, _ in graphs:
+            vc.data.copy_(base)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            graphs[1][0].replay()
+        graphs[0][0].replay()
+        torch.cuda.synchronize()
+        for g, vc, out in graphs:
+            assert torch.equal(out, want) and torch.equal(vc.data, ref.data), f"replay {rep}"
