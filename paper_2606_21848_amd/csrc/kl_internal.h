@@ -281,6 +281,7 @@ struct ScoredParams {
   void* dv;
 };
 hipError_t launch_scored_forward(const ScoredParams& p, hipStream_t stream);
+hipError_t launch_scored_forward_bf16(const ScoredParams& p, hipStream_t stream);
 hipError_t launch_scored_backward(const ScoredParams& p, hipStream_t stream);
 
 // Most drafted tokens per sequence: a token's row of the tree is one 64-bit word.

@@ -1,0 +1,112 @@
+// What the scored-attention kernels share: the seen ranges of query rows, and the
+// score of a pair as a linear form of one number per pair.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "kl_device.h"
+#include "kl_internal.h"
+
+namespace kl {
+
+constexpr float kScoredLog2e = 1.4426950408889634f;
+constexpr float kScoredLn2 = 0.69314718055994531f;
+
+// The value rows [lo, hi) that query row i sees, within [0, N); an empty range is {0, 0}.
+struct SeenRange {
+  int lo, hi;
+};
+__device__ __forceinline__ SeenRange seen_range(const ScoredParams& p, int b, int i) {
+  const size_t r = (size_t)b * p.N + i;
+  const int lo = p.first ? max(p.first[r], 0) : 0;
+  const int hi = p.last ? min(p.last[r], p.N) : (p.causal ? i + 1 : p.N);
+  return lo < hi ? SeenRange{lo, hi} : SeenRange{0, 0};
+}
+
+// What a set of rows sees: rows outside [any_lo, any_hi) are seen by none of them, rows
+// inside [all_lo, all_hi) by all. Of no rows, or of rows that see nothing, any is empty;
+// a row that sees nothing leaves all empty.
+struct SeenBounds {
+  int any_lo = 0x7fffffff, any_hi = 0, all_lo = 0, all_hi = 0x7fffffff;
+  __device__ __forceinline__ void add(SeenRange s) {
+    if (s.lo < s.hi) {
+      any_lo = min(any_lo, s.lo);
+      any_hi = max(any_hi, s.hi);
+    }
+    all_lo = max(all_lo, s.lo);
+    all_hi = min(all_hi, s.hi);
+  }
+  // Over the lanes that differ in the bits of `mask`; all of them get the result.
+  __device__ __forceinline__ void over_lanes(int mask) {
+    for (int o = 1; o <= mask; o <<= 1) {
+      if (!(o & mask)) continue;
+      any_lo = min(any_lo, __shfl_xor(any_lo, o));
+      any_hi = max(any_hi, __shfl_xor(any_hi, o));
+      all_lo = max(all_lo, __shfl_xor(all_lo, o));
+      all_hi = min(all_hi, __shfl_xor(all_hi, o));
+    }
+  }
+  // The same in scalar registers, once every lane holds the same.
+  __device__ __forceinline__ void make_uniform() {
+    any_lo = __builtin_amdgcn_readfirstlane(any_lo);
+    any_hi = __builtin_amdgcn_readfirstlane(any_hi);
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+  }
+};
+
+// x = cap tanh(z / cap) - slope dist in log2 units, from the dot product s (z = scale s).
+// A pair is first turned into one number k with x = A k + C:
+//   plain       k = s,                           A = scale log2 e,    C = 0
+//   cap         k = 1 / (1 + exp(2 z / cap)),    A = -2 cap log2 e,   C = cap log2 e
+//               (tanh(y) = 1 - 2 / (1 + exp(2 y)))
+//   with bias   k = x itself,                    A = 1,               C = 0
+// so that the shift by the row's maximum costs no operation of its own: the maximum
+// is taken over k (its minimum where A < 0) and the weight is 2^(A k + (C - m)).
+// d x / d z = 1 - tanh^2 = 4 k (1 - k) for the capped forms.
+template <bool CAP, bool BIAS>
+struct ScoreForm {
+  static constexpr bool kFalling = CAP && !BIAS;  // a larger k is a smaller score
+  float scale2;       // scale log2 e
+  float cap2, twice;  // cap log2 e; 2 scale log2 e / cap
+  float slope2;       // slope log2 e
+  __device__ __forceinline__ ScoreForm(float scale, float cap, float slope)
+      : scale2(scale * kScoredLog2e), cap2(cap * kScoredLog2e),
+        twice(CAP ? 2.f * scale * kScoredLog2e / cap : 0.f), slope2(slope * kScoredLog2e) {}
+  __device__ __forceinline__ float A() const { return BIAS ? 1.f : CAP ? -2.f * cap2 : scale2; }
+  __device__ __forceinline__ float C() const { return CAP && !BIAS ? cap2 : 0.f; }
+  static __device__ __forceinline__ float unseen() { return kFalling ? INFINITY : -INFINITY; }
+  // 1 / (1 + exp(2 z / cap)) for the capped forms.
+  __device__ __forceinline__ float bent(float s) const {
+    return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * twice));
+  }
+  __device__ __forceinline__ float key(float s, float dist) const {
+    float k = s;
+    if constexpr (CAP) k = bent(s);
+    if constexpr (BIAS) {
+      k = CAP ? fmaf(k, -2.f * cap2, cap2) : k * scale2;
+      k = fmaf(-slope2, fabsf(dist), k);
+    }
+    return k;
+  }
+  // The better of two keys.
+  static __device__ __forceinline__ float best(float a, float b) {
+    return kFalling ? fminf(a, b) : fmaxf(a, b);
+  }
+  // x - m from a key, with shift = C - m.
+  __device__ __forceinline__ float shifted(float k, float shift) const {
+    return BIAS ? k + shift : fmaf(A(), k, shift);
+  }
+};
+
+__device__ __forceinline__ bool not_finite(float x) {
+  return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u;
+}
+
+// Two bf16 in a word, those that are not finite replaced by zero.
+__device__ __forceinline__ uint32_t finite_or_zero(uint32_t w) {
+  return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) |
+         ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+}
+
+}  // namespace kl

@@ -1,0 +1,362 @@
+// Scored keyless attention, bf16 forward on the matrix cores: the keyless attention
+// (S^T = V Q~^T, then O^T += V^T P^T from one tile of values in LDS) with a tanh cap
+// and a distance bias on the scores and a range of seen value rows per query.
+//
+// A workgroup (4 waves) owns 64 QB query rows of one head, a wave 16 QB of them. It
+// walks the 64-row value tiles that any of its rows sees, in order, three in flight
+// (direct-to-LDS copies); a wave passes over a tile that none of its rows sees, and
+// masks only in tiles that some of its rows see in part. Each lane keeps the ranges
+// of its QB queries in registers, so documents, prefixes, windows and padding cost
+// what the causal mask costs.
+//
+// The routed queries are not multiplied by the scale (that would round them once
+// more): the scale joins the exponent's multiply-add. The weights' sum is taken from
+// the unrounded weights, in fp32, since the backward pass forms P from it.
+
+#include <type_traits>
+
+#include "attn_tile.h"
+#include "scored_device.h"
+
+namespace kl {
+namespace {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) unsigned char lds_u8;
+
+constexpr int kThreads = 256;
+constexpr int kTileRows = 64;  // value rows per tile
+constexpr int kStages = 3;     // tiles in LDS
+constexpr int kSchedMfma = 0x008, kSchedDsRead = 0x100;
+constexpr float kLazy = 8.f;   // the reference moves when a score exceeds it by 2^8
+
+// The online softmax of QB 16-query blocks over NB 16-row blocks of values: sc holds
+// the dot products on entry (lane: query fr of block qb, rows 16 kb + 4 grp + r of the
+// tile from row j0) and the weights on return. `edge` (uniform): some row is not seen
+// by some query; returns whether a pair that is not seen has a product that is not
+// finite (uniform). Its value row is then not finite, and 0 times it would not be
+// either: the caller takes the values that are not finite as zeros, and a query that
+// sees such a product gets NaN as its score here, and with it as its result.
+template <int D, int NB, int QB, class Form>
+__device__ __forceinline__ bool soften(const Form& form, f32x4_t (&sc)[NB][QB], f32x4_t (&o)[D / 16][QB],
+                                       float (&m)[QB], float (&l)[QB], const SeenRange (&seen)[QB],
+                                       int j0, int q0, int fr, int grp, bool edge) {
+  bool bad = false;
+  if (edge) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int j = j0 + kb * 16 + grp * 4 + r;
+          const bool out = j < seen[qb].lo || j >= seen[qb].hi;
+          bad |= out && not_finite(sc[kb][qb][r]);
+        }
+    bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+    if (bad) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (not_finite(sc[kb][qb][r])) sc[kb][qb][r] = __builtin_nanf("");
+    }
+  }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const float d0 = (float)(q0 + qb * 16 + fr - j0 - grp * 4);
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sc[kb][qb][r] = form.key(sc[kb][qb][r], d0 - (float)(kb * 16 + r));
+  }
+  if (edge) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int j = j0 + kb * 16 + grp * 4 + r;
+          if (j < seen[qb].lo || j >= seen[qb].hi) sc[kb][qb][r] = Form::unseen();
+        }
+  }
+  float top[QB];  // this lane's best score per query
+  bool grow = false;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    float k = sc[0][qb][0];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) k = Form::best(k, sc[kb][qb][r]);
+    top[qb] = fmaf(form.A(), k, form.C());
+    grow |= top[qb] > m[qb] + kLazy;
+  }
+  if (__builtin_amdgcn_ballot_w64(grow)) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      float t = fmaxf(top[qb], __shfl_xor(top[qb], 16));
+      t = fmaxf(t, __shfl_xor(t, 32));
+      const float mn = t > m[qb] + kLazy ? t : m[qb];
+      const float alpha = m[qb] == -INFINITY ? 0.f : fast_exp2(m[qb] - mn);
+      l[qb] *= alpha;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) o[i][qb] *= alpha;
+      m[qb] = mn;
+    }
+  }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const float shift = form.C() - (m[qb] == -INFINITY ? 0.f : m[qb]);
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sc[kb][qb][r] = fast_exp2(form.shifted(sc[kb][qb][r], shift));
+      l[qb] += (sc[kb][qb][0] + sc[kb][qb][1]) + (sc[kb][qb][2] + sc[kb][qb][3]);
+    }
+  }
+  return bad;
+}
+
+__device__ __forceinline__ bf16x8_t finite_or_zero(bf16x8_t v) {
+  u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int x = 0; x < 4; ++x) w[x] = kl::finite_or_zero(w[x]);
+  return __builtin_bit_cast(bf16x8_t, w);
+}
+
+__device__ __forceinline__ bf16x8_t pack8(f32x4_t a, f32x4_t b) {
+  return __builtin_bit_cast(bf16x8_t, u32x4{pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]),
+                                            pack2(b[2], b[3])});
+}
+
+// Column block db of the value rows of one 32-row step, transposed: rows 4 grp .. + 3
+// and 16 + 4 grp .. + 3 of column 16 db + fr.
+template <int ROW>
+__device__ __forceinline__ bf16x8_t value_columns(int at) {
+  const lds_u8* src = (const lds_u8*)(uintptr_t)(uint32_t)at;
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)src);
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(src + 16 * ROW));
+  return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+template <int D, int QB, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p) {
+  using T = AttnTile<D, kTileRows>;
+  using Form = ScoreForm<CAP, BIAS>;
+  constexpr int WQ = 16 * QB, BQ = 4 * WQ, KS = D / 32, DB = D / 16;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ int s_any[4][2];
+  // Groups vary fastest, then a group's heads: consecutive workgroups go to different
+  // XCDs, so where G is a multiple of 8 the heads that read one group's values share
+  // an XCD's L2. The last query tiles (under the causal mask the heaviest) start first.
+  const int R = p.H / p.G;
+  const int g = blockIdx.x % p.G, h = g * R + blockIdx.x / p.G % R;
+  const int ntq = (p.N + BQ - 1) / BQ;
+  const long tile_id = blockIdx.x / p.H;
+  const int b = (int)(tile_id % p.B), qt = ntq - 1 - (int)(tile_id / p.B);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, grp = lane >> 4;
+  const int q0 = qt * BQ + wave * WQ;
+
+  SeenRange seen[QB];
+  SeenBounds sb;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    seen[qb] = seen_range(p, b, min(q0 + qb * 16 + fr, p.N - 1));
+    sb.add(seen[qb]);
+  }
+  sb.over_lanes(15);
+  sb.make_uniform();
+  if (q0 >= p.N) sb.any_lo = sb.any_hi = 0;  // rows past the end: this wave only copies
+  if (lane == 0) {
+    s_any[wave][0] = sb.any_hi > sb.any_lo ? sb.any_lo : 0x7fffffff;
+    s_any[wave][1] = sb.any_hi;
+  }
+  __syncthreads();
+  int lo = s_any[0][0], hi = s_any[0][1];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) {
+    lo = min(lo, s_any[w][0]);
+    hi = max(hi, s_any[w][1]);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  const int t0 = lo < hi ? lo / kTileRows : 0;
+  const int ntiles = lo < hi ? (hi + kTileRows - 1) / kTileRows - t0 : 0;
+
+  const size_t row_bytes = (size_t)p.G * D * 2;
+  const unsigned char* gV = static_cast<const unsigned char*>(p.v) + ((size_t)b * p.N * p.G + g) * D * 2;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
+  // Copy c of this wave fills tile rows (4 c + wave) RPC .. + RPC - 1.
+  constexpr int RPC = 1024 / T::ROW;
+  uint32_t chunk[T::COPIES];
+#pragma unroll
+  for (int c = 0; c < T::COPIES; ++c)
+    chunk[c] = (uint32_t)(T::swz((c * 4 + wave) * RPC + lane / T::CHUNKS, lane % T::CHUNKS) * 16);
+  const uint32_t lane_row = (uint32_t)(lane / T::CHUNKS) * (uint32_t)row_bytes;
+  auto issue = [&](int t, int stage) {
+    const int j0 = (t0 + t) * kTileRows;
+    const uint32_t st = lds0 + stage * T::BYTES;
+    if (j0 + kTileRows <= p.N) {
+      const unsigned char* tb = gV + (size_t)j0 * row_bytes;
+#pragma unroll
+      for (int c = 0; c < T::COPIES; ++c)
+        copy_to_lds(tb + (size_t)((c * 4 + wave) * RPC) * row_bytes, lane_row + chunk[c],
+                    st + (c * 4 + wave) * 1024);
+    } else {
+#pragma unroll
+      for (int c = 0; c < T::COPIES; ++c) {
+        const int r0 = j0 + (c * 4 + wave) * RPC, r0c = min(r0, p.N - 1);
+        const int rl = min(r0 + lane / T::CHUNKS, p.N - 1) - r0c;
+        copy_to_lds(gV + (size_t)r0c * row_bytes, (uint32_t)(rl * row_bytes) + chunk[c],
+                    st + (c * 4 + wave) * 1024);
+      }
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s)
+    if (s < ntiles) issue(s, s);
+
+  bf16x8_t qf[QB][KS];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const uint16_t* src = static_cast<const uint16_t*>(p.q) +
+                          (((size_t)b * p.N + min(q0 + qb * 16 + fr, p.N - 1)) * p.H + h) * D + grp * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      qf[qb][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(src + ks * 32));
+  }
+  const Form form(p.scale, p.cap, BIAS ? p.slopes[h] : 0.f);
+  f32x4_t o[DB][QB];
+  float m[QB], l[QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    m[qb] = -INFINITY;
+    l[qb] = 0.f;
+#pragma unroll
+    for (int i = 0; i < DB; ++i) o[i][qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const FragOffsets<D> fo(fr, grp);
+  // The wait for the queries is taken here, where the first tiles are awaited anyway.
+  KL_WAIT_VMCNT(0);
+  int stage = 0;
+  for (int t = 0; t < ntiles; ++t) {
+    if (t + 1 < ntiles) KL_WAIT_VMCNT((kStages - 2) * T::COPIES);
+    else KL_WAIT_VMCNT(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage refilled below has been read
+    __syncthreads();
+    if (t + kStages - 1 < ntiles) issue(t + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+    const int j0 = (t0 + t) * kTileRows;
+    const int tile = (int)lds0 + stage * T::BYTES;
+    stage = stage == kStages - 1 ? 0 : stage + 1;
+    if (j0 >= sb.any_hi || j0 + kTileRows <= sb.any_lo) continue;
+    const FragOffsets<D> fi = fo.at(tile);
+    f32x4_t sc[4][QB];
+    {
+      int offS[KS];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) offS[ks] = fi.s(ks);
+      bf16x8_t sa[2][KS];
+      auto rows = [&](int kb, int ks) {
+        return *(const __attribute__((address_space(3))) bf16x8_t*)(uintptr_t)(
+            uint32_t)(offS[ks] + kb * 16 * T::ROW);
+      };
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) sa[0][ks] = rows(0, ks);
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) {
+        if (kb + 1 < 4) {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) sa[(kb + 1) & 1][ks] = rows(kb + 1, ks);
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+            sc[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                sa[kb & 1][ks], qf[qb][ks], ks == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[kb][qb], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(kSchedDsRead, KS, 0);
+#pragma unroll
+      for (int kb = 0; kb < 3; ++kb) {
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, KS, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, KS * QB, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, KS * QB, 0);
+    }
+    const bool edge = j0 < sb.all_lo || j0 + kTileRows > sb.all_hi;
+    const bool bad = soften<D, 4, QB>(form, sc, o, m, l, seen, j0, q0, fr, grp, edge);
+    int offT[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) offT[db] = fi.t(db);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      bf16x8_t pf[QB], av[DB];
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) pf[qb] = pack8(sc[2 * ks][qb], sc[2 * ks + 1][qb]);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) av[db] = value_columns<T::ROW>(offT[db] + ks * 32 * T::ROW);
+      if (bad) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) av[db] = finite_or_zero(av[db]);
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+          o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[db], pf[qb], o[db][qb], 0, 0, 0);
+    }
+  }
+
+  // Lane holds O[q][16 db + 4 grp + r]; the sums of a query lie over its four lane groups.
+  uint16_t* __restrict__ O = static_cast<uint16_t*>(p.out);
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int q = q0 + qb * 16 + fr;
+    float sum = l[qb] + __shfl_xor(l[qb], 16);
+    sum += __shfl_xor(sum, 32);
+    if (q >= p.N) continue;
+    const bool none = seen[qb].lo >= seen[qb].hi;
+    const float inv = none ? 0.f : 1.f / sum;
+    if (p.lse && grp == 0)
+      p.lse[((size_t)b * p.H + h) * p.N + q] = none ? -INFINITY : (m[qb] + __log2f(sum)) * kScoredLn2;
+    const size_t at = (((size_t)b * p.N + q) * p.H + h) * D + grp * 4;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const f32x4_t x = o[db][qb] * inv;
+      if (p.out_f32) *reinterpret_cast<f32x4_t*>(p.out_f32 + at + db * 16) = x;
+      *reinterpret_cast<u32x2*>(O + at + db * 16) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+    }
+  }
+}
+
+template <int D, int QB, bool CAP, bool BIAS>
+hipError_t launch_qb(const ScoredParams& p, hipStream_t st) {
+  constexpr int BQ = 64 * QB, lds = kStages * AttnTile<D, kTileRows>::BYTES;
+  const dim3 grid((unsigned)p.H * p.B * ((p.N + BQ - 1) / BQ));
+  hipLaunchKernelGGL((scored_fwd_kernel<D, QB, CAP, BIAS>), grid, dim3(kThreads), lds, st, p);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_d(const ScoredParams& p, hipStream_t st) {
+  if (p.cap > 0.f) return p.slopes ? launch_qb<D, 2, true, true>(p, st) : launch_qb<D, 2, true, false>(p, st);
+  return p.slopes ? launch_qb<D, 2, false, true>(p, st) : launch_qb<D, 2, false, false>(p, st);
+}
+
+}  // namespace
+
+hipError_t launch_scored_forward_bf16(const ScoredParams& p, hipStream_t st) {
+  return p.D == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);
+}
+
+}  // namespace kl

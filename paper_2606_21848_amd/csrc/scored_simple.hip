@@ -247,6 +247,7 @@ hipError_t pick(kl_dtype dtype, int D, F f) {
 }  // namespace
 
 hipError_t launch_scored_forward(const ScoredParams& p, hipStream_t stream) {
+  if (p.dtype == KL_BF16) return launch_scored_forward_bf16(p, stream);
   const dim3 grid((unsigned)p.H * p.B * ((p.N + kRows - 1) / kRows));
   return pick(p.dtype, p.D, [&](auto t, auto d) {
     hipLaunchKernelGGL((forward_kernel<decltype(t), decltype(d)::value>), grid, dim3(256), 0, stream, p);
