@@ -1282,6 +1282,25 @@ int check_scored_args(const char* who, const void* q, const void* v, const void*
   return KL_OK;
 }
 
+// Workspace of keyless_scored_backward: the row sums, and for bf16 what each row and
+// each 64-row tile sees and the fp32 partial sums of dv over S splits.
+struct ScoredBwdLayout {
+  size_t lo, hi, tiles, part, total;
+  int S;
+};
+ScoredBwdLayout scored_bwd_layout(int B, int N, int H, int G, int d_head, kl_dtype dtype) {
+  ScoredBwdLayout L{};
+  L.S = 1;
+  L.lo = L.total = bwd_rows_bytes(B, N, H);
+  if (dtype != KL_BF16) return L;
+  L.S = kl::attn_bwd_splits(B, N, H, G, true);
+  L.hi = L.lo + align256((size_t)B * N * sizeof(int));
+  L.tiles = L.hi + align256((size_t)B * N * sizeof(int));
+  L.part = L.tiles + align256((size_t)B * ((N + 63) / 64) * 4 * sizeof(int));
+  L.total = L.part + (L.S > 1 ? align256((size_t)L.S * B * N * G * d_head * sizeof(float)) : 0);
+  return L;
+}
+
 kl::ScoredParams scored_params(const void* q, const void* v, const kl_scoring* sc, int B, int N,
                                int H, int G, int d_head, float scale, kl_dtype dtype) {
   kl::ScoredParams p{};
@@ -1323,7 +1342,7 @@ int keyless_scored_forward(const void* q_routed, const void* v, const kl_scoring
 size_t keyless_scored_backward_workspace_size(int B, int N, int H, int G, int d_head,
                                               kl_dtype dtype) {
   if (B < 0 || N < 0 || H <= 0 || G <= 0 || H % G != 0 || d_head <= 0 || !dtype_ok(dtype)) return 0;
-  return bwd_rows_bytes(B, N, H);
+  return scored_bwd_layout(B, N, H, G, d_head, dtype).total;
 }
 
 int keyless_scored_backward(const void* q_routed, const void* v, const void* out,
@@ -1349,7 +1368,14 @@ int keyless_scored_backward(const void* q_routed, const void* v, const void* out
   p.out_f32 = const_cast<float*>(out_f32);
   p.out_in = out;
   p.dout = dout;
-  p.Dd = static_cast<float*>(ws);
+  const ScoredBwdLayout L = scored_bwd_layout(B, N, H, G, d_head, dtype);
+  char* w = static_cast<char*>(ws);
+  p.Dd = reinterpret_cast<float*>(w);
+  p.row_lo = reinterpret_cast<int*>(w + L.lo);
+  p.row_hi = reinterpret_cast<int*>(w + L.hi);
+  p.tile_sees = w + L.tiles;
+  p.S = L.S;
+  p.part = reinterpret_cast<float*>(w + L.part);
   p.dq = dq_routed;
   p.dv = dv;
   return hip_status(kl::launch_scored_backward(p, static_cast<hipStream_t>(stream)), who);

@@ -279,10 +279,16 @@ struct ScoredParams {
   float* Dd;             // [B, H, N] scratch: rowsum(P * dP)
   void* dq;
   void* dv;
+  int* row_lo;           // [B, N] scratch: what each query row sees (bf16)
+  int* row_hi;
+  void* tile_sees;       // [B, ceil(N / 64), 4] int scratch: rows seen by any, by all rows of a tile (bf16)
+  int S;                 // splits of the dV sums, 1 for none (bf16)
+  float* part;           // their fp32 partial sums [S, B, N, G, D]
 };
 hipError_t launch_scored_forward(const ScoredParams& p, hipStream_t stream);
 hipError_t launch_scored_forward_bf16(const ScoredParams& p, hipStream_t stream);
 hipError_t launch_scored_backward(const ScoredParams& p, hipStream_t stream);
+hipError_t launch_scored_backward_bf16(const ScoredParams& p, hipStream_t stream);
 
 // Most drafted tokens per sequence: a token's row of the tree is one 64-bit word.
 constexpr int kMaxDrafts = 64;

@@ -1,0 +1,579 @@
+// Scored keyless attention, bf16 backward on the matrix cores. Per batch and head, with
+// x the capped and biased score and z the plain one:
+//   P   = exp(x - lse),  dP = dO V^T,  Dd = rowsum(dO * O)
+//   dx  = P * (dP - Dd),  dz = dx (1 - tanh^2(z / cap))
+//   dQ~ = scale dz V
+//   dV  = P^T dO + scale dz^T Q~   (both roles of the values, every head of the group)
+//
+// scored_dq_kernel (one workgroup per 128 query rows and head; value tiles stream
+// through LDS, queries and dO stay in registers) publishes for the second kernel what
+// each query row and each 64-row query tile sees, and Dd. scored_dv_kernel (one
+// workgroup per 192 value rows and group; tiles of Q~ and dO stream through LDS, the
+// values stay in registers) walks the query tiles that see any of its rows, for every
+// head of its group, and masks only in tiles that see them in part. No atomics.
+// Scores come out with one query per lane in the first kernel and one value row per
+// lane in the second, so that in both the weights are the next product's second operand
+// as they stand. Queries and weights are not multiplied by the scale before a rounding.
+
+#include <algorithm>
+
+#include "attn_tile.h"
+#include "scored_device.h"
+
+namespace kl {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTileRows = 64;
+constexpr int kStages = 3;           // value tiles in LDS (dQ~)
+constexpr int QB = 2, BQ = 64 * QB;  // 16-row query blocks per wave, query rows per workgroup (dQ~)
+constexpr int KVB = 3, BKV = 64 * KVB;  // value blocks per wave, value rows per workgroup (dV)
+
+// One 4-byte-per-lane copy from global memory straight into LDS.
+__device__ __forceinline__ void copy_dword_to_lds(const void* gbase, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+               :
+               : "v"(voff), "s"(gbase), "s"(lds)
+               : "memory", "m0");
+}
+
+// P and dz (times `scale4` / 4 where it is not 1) of one pair: `k` the key, `dp` dP - Dd.
+// shift = C - lse in log2 units.
+template <class Form, bool CAP, bool BIAS>
+__device__ __forceinline__ void weigh(const Form& form, float s, float dist, float dp, float shift,
+                                      float scale, float& w, float& dz) {
+  if constexpr (CAP) {
+    const float k = form.bent(s);
+    float x = k;
+    if constexpr (BIAS) x = fmaf(-form.slope2, fabsf(dist), fmaf(k, -2.f * form.cap2, form.cap2));
+    w = fast_exp2(form.shifted(x, shift));
+    const float k4 = k * (4.f * scale);
+    dz = w * dp * fmaf(-k4, k, k4);  // 1 - tanh^2 = 4 k (1 - k)
+  } else {
+    w = fast_exp2(form.shifted(form.key(s, dist), shift));
+    dz = w * dp * scale;
+  }
+}
+
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) {
+  using T = AttnTile<D, kTileRows>;
+  using Form = ScoreForm<CAP, BIAS>;
+  constexpr int KS = D / 32, DB = D / 16;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ int s_sees[4][4];
+  const HeadTile ht(p, BQ);
+  const int h = ht.h, g = ht.g, b = ht.b, qt = ht.qt;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, grp = lane >> 4;
+  const int q0 = qt * BQ + wave * 16 * QB;
+
+  // What the rows see; the first head's workgroup publishes it (rows past the end see
+  // nothing there, so that a query tile with a tail counts as seen in part).
+  SeenRange seen[QB];
+  SeenBounds sb, pub;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int q = q0 + qb * 16 + fr;
+    seen[qb] = seen_range(p, b, min(q, p.N - 1));
+    sb.add(seen[qb]);
+    pub.add(q < p.N ? seen[qb] : SeenRange{0, 0});
+    if (h == 0 && grp == 0 && q < p.N) {
+      p.row_lo[(size_t)b * p.N + q] = seen[qb].lo;
+      p.row_hi[(size_t)b * p.N + q] = seen[qb].hi;
+    }
+  }
+  sb.over_lanes(15);
+  pub.over_lanes(15);
+  sb.make_uniform();
+  if (q0 >= p.N) sb.any_lo = sb.any_hi = 0;
+  if (lane == 0) {
+    s_sees[wave][0] = pub.any_lo;
+    s_sees[wave][1] = pub.any_hi;
+    s_sees[wave][2] = pub.all_lo;
+    s_sees[wave][3] = pub.all_hi;
+  }
+  __syncthreads();
+  if (h == 0 && threadIdx.x < 2) {
+    const int x = 2 * threadIdx.x, tile = 2 * qt + threadIdx.x, tiles = (p.N + 63) / 64;
+    if (tile < tiles) {
+      const i32x4 v{min(s_sees[x][0], s_sees[x + 1][0]), max(s_sees[x][1], s_sees[x + 1][1]),
+             max(s_sees[x][2], s_sees[x + 1][2]), min(s_sees[x][3], s_sees[x + 1][3])};
+      static_cast<i32x4*>(p.tile_sees)[(size_t)b * tiles + tile] = v;
+    }
+  }
+  int lo = s_sees[0][0], hi = s_sees[0][1];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) {
+    lo = min(lo, s_sees[w][0]);
+    hi = max(hi, s_sees[w][1]);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  const int t0 = lo < hi ? lo / kTileRows : 0;
+  const int ntiles = lo < hi ? (hi + kTileRows - 1) / kTileRows - t0 : 0;
+
+  const size_t row_bytes = (size_t)p.G * D * 2;
+  const unsigned char* gV = static_cast<const unsigned char*>(p.v) + ((size_t)b * p.N * p.G + g) * D * 2;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
+  const TileCopy<D> cp(wave, lane, row_bytes);
+  auto issue = [&](int t, int stage) {
+    cp.issue(gV, row_bytes, (t0 + t) * kTileRows, p.N, wave, lane, lds0 + stage * T::BYTES);
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s)
+    if (s < ntiles) issue(s, s);
+
+  // Query row q0 + 16 qb + fr, columns 32 ks + 8 grp .. + 7, of Q~ and dO. dP starts from
+  // -Dd; Dd comes from the forward's fp32 output when it was kept, else it is there.
+  bf16x8_t qf[QB][KS], df[QB][KS];
+  f32x4_t ndd[QB], acc[DB][QB];
+  float shift[QB];
+  const Form form(p.scale, p.cap, BIAS ? p.slopes[h] : 0.f);
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int q = q0 + qb * 16 + fr, qq = min(q, p.N - 1);
+    const size_t at = (((size_t)b * p.N + qq) * p.H + h) * D + grp * 8;
+    const size_t row = ((size_t)b * p.H + h) * p.N + qq;
+    float d0 = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[qb][ks] = __builtin_bit_cast(
+          bf16x8_t, *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + at + ks * 32));
+      const u32x4 gw = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.dout) + at + ks * 32);
+      df[qb][ks] = __builtin_bit_cast(bf16x8_t, gw);
+      if (p.out_f32) {
+        const f32x4_t o0 = *reinterpret_cast<const f32x4_t*>(p.out_f32 + at + ks * 32);
+        const f32x4_t o1 = *reinterpret_cast<const f32x4_t*>(p.out_f32 + at + ks * 32 + 4);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          d0 = fmaf(bf16_lo(gw[j]), o0[2 * j], fmaf(bf16_hi(gw[j]), o0[2 * j + 1], d0));
+          d0 = fmaf(bf16_lo(gw[j + 2]), o1[2 * j], fmaf(bf16_hi(gw[j + 2]), o1[2 * j + 1], d0));
+        }
+      }
+    }
+    if (p.out_f32) {
+      d0 += __shfl_xor(d0, 16);
+      d0 += __shfl_xor(d0, 32);
+      if (grp == 0 && q < p.N) p.Dd[row] = d0;
+    } else {
+      d0 = p.Dd[row];
+    }
+    ndd[qb] = f32x4_t{-d0, -d0, -d0, -d0};
+    shift[qb] = form.C() - p.lse[row] * kScoredLog2e;
+#pragma unroll
+    for (int i = 0; i < DB; ++i) acc[i][qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const FragOffsets<D> fo(fr, grp);
+  KL_WAIT_VMCNT(0);
+  int stage = 0;
+  for (int t = 0; t < ntiles; ++t) {
+    if (t + 1 < ntiles) KL_WAIT_VMCNT((kStages - 2) * T::COPIES);
+    else KL_WAIT_VMCNT(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage refilled below has been read
+    __syncthreads();
+    if (t + kStages - 1 < ntiles) issue(t + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+    const int j0 = (t0 + t) * kTileRows;
+    const FragOffsets<D> fi = fo.at(lds0 + stage * T::BYTES);
+    stage = stage == kStages - 1 ? 0 : stage + 1;
+    if (j0 >= sb.any_hi || j0 + kTileRows <= sb.any_lo) continue;
+    const bool edge = j0 < sb.all_lo || j0 + kTileRows > sb.all_hi;
+    // One 32-row step at a time, which keeps half of the tile's scores live.
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      f32x4_t sc[2][QB], dp[2][QB];
+      bf16x8_t va[2][KS];
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+        for (int kd = 0; kd < KS; ++kd) va[hh][kd] = lds_rows(fi.s(kd) + (2 * ks + hh) * 16 * T::ROW);
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+        for (int kd = 0; kd < KS; ++kd)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) {
+            sc[hh][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                va[hh][kd], qf[qb][kd], kd == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[hh][qb], 0, 0, 0);
+            dp[hh][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[hh][kd], df[qb][kd],
+                                                                 kd == 0 ? ndd[qb] : dp[hh][qb], 0, 0, 0);
+          }
+      __builtin_amdgcn_sched_group_barrier(kSchedDsRead, KS, 0);
+#pragma unroll
+      for (int kd = 0; kd < KS; ++kd) {
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2 * QB, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2 * QB * KS, 0);
+      // Lane: rows jl + 16 hh + r of query q0 + 16 qb + fr.
+      const int jl = j0 + 32 * ks + grp * 4;
+      auto unseen = [&](int qb, int hh, int r) {
+        const int j = jl + hh * 16 + r;
+        return j < seen[qb].lo || j >= seen[qb].hi;
+      };
+      bool bad = false;  // see the forward: values that a query must not see are not finite
+      if (edge) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              bad |= unseen(qb, hh, r) && (not_finite(sc[hh][qb][r]) || not_finite(dp[hh][qb][r]));
+        bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+        if (bad) {
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (not_finite(sc[hh][qb][r])) dp[hh][qb][r] = __builtin_nanf("");
+        }
+      }
+      bf16x8_t pf[QB];
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        const float dist = (float)(q0 + qb * 16 + fr - jl);
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float w, dz;
+            weigh<Form, CAP, BIAS>(form, sc[hh][qb][r], dist - (float)(hh * 16 + r), dp[hh][qb][r],
+                                   shift[qb], 1.f, w, dz);
+            sc[hh][qb][r] = dz;
+          }
+      }
+      if (edge) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (unseen(qb, hh, r)) sc[hh][qb][r] = 0.f;
+      }
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) pf[qb] = pack8(sc[0][qb], sc[1][qb]);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        bf16x8_t a = lds_columns<T::ROW>(fi.t(db) + ks * 32 * T::ROW);
+        if (bad) a = finite_or_zero(a);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+          acc[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf[qb], acc[db][qb], 0, 0, 0);
+      }
+    }
+  }
+  // Lane holds dQ~^T[16 db + 4 grp + r][q].
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int q = q0 + qb * 16 + fr;
+    if (q >= p.N) continue;
+    uint16_t* dst = static_cast<uint16_t*>(p.dq) + (((size_t)b * p.N + q) * p.H + h) * D + grp * 4;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const f32x4_t x = acc[db][qb] * p.scale;
+      *reinterpret_cast<u32x2*>(dst + db * 16) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+    }
+  }
+}
+
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) {
+  using T = AttnTile<D, kTileRows>;
+  using Form = ScoreForm<CAP, BIAS>;
+  constexpr int KS = D / 32, DB = D / 16;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ int s_first[4], s_last[4];
+  const int R = p.H / p.G, g = blockIdx.x % p.G;
+  const int kvt = (int)(blockIdx.x / p.G / (p.B * p.S));
+  const int bs = (int)(blockIdx.x / p.G % (p.B * p.S)), b = bs % p.B, split = bs / p.B;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, grp = lane >> 4;
+  const int wg0 = kvt * BKV, kv0 = wg0 + wave * 16 * KVB;
+
+  // The query tiles from the first to the last that sees one of the workgroup's rows.
+  const int tiles = (p.N + 63) / 64;
+  const i32x4* sees = static_cast<const i32x4*>(p.tile_sees) + (size_t)b * tiles;
+  int first = tiles, last = 0;
+  for (int t = threadIdx.x; t < tiles; t += kThreads) {
+    const i32x4 s = sees[t];
+    if (s.x < wg0 + BKV && s.y > wg0) {
+      first = min(first, t);
+      last = max(last, t + 1);
+    }
+  }
+  for (int o = 1; o < 64; o <<= 1) {
+    first = min(first, __shfl_xor(first, o));
+    last = max(last, __shfl_xor(last, o));
+  }
+  if (lane == 0) {
+    s_first[wave] = first;
+    s_last[wave] = last;
+  }
+
+  bf16x8_t vf[KVB][KS];
+#pragma unroll
+  for (int kb = 0; kb < KVB; ++kb) {
+    const int kv = min(kv0 + kb * 16 + fr, p.N - 1);
+    const uint16_t* sv = static_cast<const uint16_t*>(p.v) + (((size_t)b * p.N + kv) * p.G + g) * D + grp * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      vf[kb][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(sv + ks * 32));
+  }
+  f32x4_t acc[DB][KVB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int kb = 0; kb < KVB; ++kb) acc[i][kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    first = min(first, s_first[w]);
+    last = max(last, s_last[w]);
+  }
+  first = __builtin_amdgcn_readfirstlane(first);
+  last = __builtin_amdgcn_readfirstlane(last);
+
+  // Work items: (head of the group, query tile) pairs, heads outermost; this
+  // workgroup's share of them where they are split. The bounds are read as scalars
+  // (an earlier kernel wrote them).
+  const int per = max(last - first, 0);
+  int it = 0, items = R * per;
+  if (p.S > 1) {
+    it = (int)((long)items * split / p.S);
+    items = (int)((long)items * (split + 1) / p.S);
+  }
+  typedef const __attribute__((address_space(4))) i32x4 const_i32x4;
+  auto bounds = [&](int i) { return ((const_i32x4*)sees)[first + i % per]; };
+  auto seek = [&](int i) {
+    for (; i < items; ++i) {
+      const i32x4 s = bounds(i);
+      if (s.x < wg0 + BKV && s.y > wg0) break;
+    }
+    return i;
+  };
+  const size_t row_bytes = (size_t)p.H * D * 2;
+  const unsigned char* gQ = static_cast<const unsigned char*>(p.q) + (size_t)b * p.N * row_bytes;
+  const unsigned char* gD = static_cast<const unsigned char*>(p.dout) + (size_t)b * p.N * row_bytes;
+  const TileCopy<D> cp(wave, lane, row_bytes);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
+  // An item's 64 rows' lse, Dd and seen ranges travel with its tiles, 256 bytes each.
+  const uint32_t rows0 = lds0 + 4 * T::BYTES;
+  auto issue = [&](int i, int stage) {
+    const int h = g * R + i / per, r0 = (first + i % per) * kTileRows;
+    const uint32_t st = lds0 + stage * 2 * T::BYTES, rs = rows0 + stage * 1024 + wave * 256;
+    cp.issue(gQ + (size_t)h * D * 2, row_bytes, r0, p.N, wave, lane, st);
+    cp.issue(gD + (size_t)h * D * 2, row_bytes, r0, p.N, wave, lane, st + T::BYTES);
+    const uint32_t off = (uint32_t)(min(r0 + lane, p.N - 1) - r0) * 4;
+    const size_t hr = ((size_t)b * p.H + h) * p.N + r0, br = (size_t)b * p.N + r0;
+    const void* src = wave == 0   ? static_cast<const void*>(p.lse + hr)
+                      : wave == 1 ? static_cast<const void*>(p.Dd + hr)
+                      : wave == 2 ? static_cast<const void*>(p.row_lo + br)
+                                  : static_cast<const void*>(p.row_hi + br);
+    copy_dword_to_lds(src, off, rs);
+  };
+  const FragOffsets<D> fo(fr, grp);
+  it = seek(it);
+  int stage = 0;
+  if (it < items) issue(it, 0);
+  while (it < items) {
+    const int next = seek(it + 1);
+    KL_WAIT_VMCNT(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (next < items) issue(next, stage ^ 1);
+    const int q0 = (first + it % per) * kTileRows, h = g * R + it / per;
+    const i32x4 s = bounds(it);
+    const FragOffsets<D> fi = fo.at(lds0 + stage * 2 * T::BYTES);
+    const int rows_it = (int)(rows0 + stage * 1024);
+    it = next;
+    stage ^= 1;
+    if (s.x >= kv0 + 16 * KVB || s.y <= kv0) continue;  // no row of the tile sees this wave's
+    // Rows past the end see nothing, so that a tile with a tail is an edge.
+    const bool edge = s.z > kv0 || s.w < kv0 + 16 * KVB;
+    const Form form(p.scale, p.cap, BIAS ? p.slopes[h] : 0.f);
+#pragma unroll
+    for (int qs = 0; qs < 2; ++qs) {
+      u32x4 wp[KVB], wz[KVB];
+      bool bad = false;  // a row that does not see a value is not finite: see the forward
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        const int qb = 2 * qs + hh;  // 16-row query block of the tile
+        f32x4_t sc[KVB], dp[KVB];
+        __builtin_amdgcn_sched_barrier(0);
+        bf16x8_t aq[KS], ad[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const int a = fi.s(ks) + qb * 16 * T::ROW;
+          aq[ks] = lds_rows(a);
+          ad[ks] = lds_rows(a + T::BYTES);
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+          for (int kb = 0; kb < KVB; ++kb) {
+            sc[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                aq[ks], vf[kb][ks], ks == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[kb], 0, 0, 0);
+            dp[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                ad[ks], vf[kb][ks], ks == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : dp[kb], 0, 0, 0);
+          }
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 4, 0);
+#pragma unroll
+        for (int ks = 0; ks + 2 < KS; ++ks) {
+          __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2 * KVB, 0);
+          __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4 * KVB, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        // Lane: query rows ql + r against value row kv0 + 16 kb + fr.
+        const int ql = q0 + qb * 16 + grp * 4, rl = rows_it + (qb * 16 + grp * 4) * 4;
+        auto row_data = [&](int which) {
+          return *(const __attribute__((address_space(3))) f32x4_t*)(uintptr_t)(uint32_t)(rl + which * 256);
+        };
+        const f32x4_t lse = row_data(0), dd = row_data(1);
+        int lo[4], hi[4];
+        if (edge) {
+          const f32x4_t a = row_data(2), z = row_data(3);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const bool live = ql + r < p.N;
+            lo[r] = live ? __float_as_int(a[r]) : 0;
+            hi[r] = live ? __float_as_int(z[r]) : 0;
+          }
+          bool odd = false;
+#pragma unroll
+          for (int kb = 0; kb < KVB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int kv = kv0 + kb * 16 + fr;
+              odd |= (kv < lo[r] || kv >= hi[r]) && (not_finite(sc[kb][r]) || not_finite(dp[kb][r]));
+            }
+          odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+          bad |= odd;
+          if (odd) {
+#pragma unroll
+            for (int kb = 0; kb < KVB; ++kb)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (not_finite(sc[kb][r]) || not_finite(dp[kb][r])) sc[kb][r] = __builtin_nanf("");
+          }
+        }
+#pragma unroll
+        for (int kb = 0; kb < KVB; ++kb) {
+          const float dist = (float)(ql - (kv0 + kb * 16 + fr));
+          float w[4], dz[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            weigh<Form, CAP, BIAS>(form, sc[kb][r], dist + (float)r, dp[kb][r] - dd[r],
+                                   fmaf(-lse[r], kScoredLog2e, form.C()), p.scale, w[r], dz[r]);
+          }
+          if (edge) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int kv = kv0 + kb * 16 + fr;
+              if (kv < lo[r] || kv >= hi[r]) w[r] = dz[r] = 0.f;
+            }
+          }
+          wp[kb][2 * hh] = pack2(w[0], w[1]);
+          wp[kb][2 * hh + 1] = pack2(w[2], w[3]);
+          wz[kb][2 * hh] = pack2(dz[0], dz[1]);
+          wz[kb][2 * hh + 1] = pack2(dz[2], dz[3]);
+        }
+      }
+      // dV^T += dO^T P + Q~^T (scale dz) over query rows 32 qs + {4 grp .., 16 + 4 grp ..}.
+      __builtin_amdgcn_sched_barrier(0);
+      bf16x8_t ad[DB], aq[DB];
+      auto rd = [&](int db) {
+        const int a = fi.t(db) + qs * 32 * T::ROW;
+        ad[db] = lds_columns<T::ROW>(a + T::BYTES);
+        aq[db] = lds_columns<T::ROW>(a);
+        if (bad) {
+          ad[db] = finite_or_zero(ad[db]);
+          aq[db] = finite_or_zero(aq[db]);
+        }
+      };
+      rd(0);
+      rd(1);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        if (db + 2 < DB) rd(db + 2);
+#pragma unroll
+        for (int kb = 0; kb < KVB; ++kb) {
+          acc[db][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              ad[db], __builtin_bit_cast(bf16x8_t, wp[kb]), acc[db][kb], 0, 0, 0);
+          acc[db][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              aq[db], __builtin_bit_cast(bf16x8_t, wz[kb]), acc[db][kb], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 8, 0);
+#pragma unroll
+      for (int db = 0; db + 2 < DB; ++db) {
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2 * KVB, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 4, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4 * KVB, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+
+  // Lane holds dV^T[16 db + 4 grp + r][kv0 + 16 kb + fr]; a split leaves its sums in
+  // fp32, laid out as dv.
+#pragma unroll
+  for (int kb = 0; kb < KVB; ++kb) {
+    const int kv = kv0 + kb * 16 + fr;
+    if (kv >= p.N) continue;
+    const size_t at = (((size_t)b * p.N + kv) * p.G + g) * D + grp * 4;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      if (p.S > 1)
+        *reinterpret_cast<f32x4_t*>(p.part + (size_t)split * p.B * p.N * p.G * D + at + db * 16) = acc[db][kb];
+      else
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.dv) + at + db * 16) =
+            u32x2{pack2(acc[db][kb][0], acc[db][kb][1]), pack2(acc[db][kb][2], acc[db][kb][3])};
+    }
+  }
+}
+
+template <int D, bool CAP, bool BIAS>
+hipError_t launch_form(const ScoredParams& p, hipStream_t st) {
+  using T = AttnTile<D, kTileRows>;
+  constexpr int dq_lds = kStages * T::BYTES;
+  constexpr int dv_lds = 4 * T::BYTES + 2048;  // two stages of Q~ and dO tiles and their rows
+  hipLaunchKernelGGL((scored_dq_kernel<D, CAP, BIAS>), dim3((unsigned)p.H * p.B * ((p.N + BQ - 1) / BQ)),
+                     dim3(kThreads), dq_lds, st, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (dv_lds > 65536) {
+    static std::atomic<uint32_t> done{0};
+    e = set_max_lds(reinterpret_cast<const void*>(scored_dv_kernel<D, CAP, BIAS>), dv_lds, done);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((scored_dv_kernel<D, CAP, BIAS>),
+                     dim3((unsigned)p.G * p.B * p.S * ((p.N + BKV - 1) / BKV)), dim3(kThreads), dv_lds, st, p);
+  e = hipGetLastError();
+  if (e != hipSuccess || p.S == 1) return e;
+  return launch_sum_partials_bf16(p.part, p.S, (size_t)p.B * p.N * p.G * D, p.dv, st);
+}
+
+template <int D>
+hipError_t launch_d(const ScoredParams& p, hipStream_t st) {
+  if (p.cap > 0.f) return p.slopes ? launch_form<D, true, true>(p, st) : launch_form<D, true, false>(p, st);
+  return p.slopes ? launch_form<D, false, true>(p, st) : launch_form<D, false, false>(p, st);
+}
+
+}  // namespace
+
+hipError_t launch_scored_backward_bf16(const ScoredParams& p, hipStream_t st) {
+  if (!p.out_f32) {  // rowsum(dO * O) from a second forward pass, which has O in fp32
+    const hipError_t e = launch_scored_forward_bf16(p, st);
+    if (e != hipSuccess) return e;
+  }
+  return p.D == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);
+}
+
+}  // namespace kl

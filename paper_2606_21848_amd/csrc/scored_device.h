@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "attn_tile.h"
 #include "kl_device.h"
 #include "kl_internal.h"
 
@@ -108,5 +109,94 @@ __device__ __forceinline__ uint32_t finite_or_zero(uint32_t w) {
   return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) |
          ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
 }
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) unsigned char lds_u8;
+
+// Instruction classes of __builtin_amdgcn_sched_group_barrier.
+constexpr int kSchedMfma = 0x008, kSchedDsRead = 0x100;
+
+__device__ __forceinline__ bf16x8_t finite_or_zero(bf16x8_t v) {
+  u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int x = 0; x < 4; ++x) w[x] = finite_or_zero(w[x]);
+  return __builtin_bit_cast(bf16x8_t, w);
+}
+
+__device__ __forceinline__ bf16x8_t pack8(f32x4_t a, f32x4_t b) {
+  return __builtin_bit_cast(bf16x8_t, u32x4{pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]),
+                                            pack2(b[2], b[3])});
+}
+
+// One 16-byte row fragment at an LDS address.
+__device__ __forceinline__ bf16x8_t lds_rows(int at) {
+  return *(const __attribute__((address_space(3))) bf16x8_t*)(uintptr_t)(uint32_t)at;
+}
+
+// One 16-column block of 32 rows, transposed: rows 4 grp .. + 3 and 16 + 4 grp .. + 3 of
+// this lane's column.
+template <int ROW>
+__device__ __forceinline__ bf16x8_t lds_columns(int at) {
+  const lds_u8* src = (const lds_u8*)(uintptr_t)(uint32_t)at;
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)src);
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(src + 16 * ROW));
+  return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// A workgroup's (4 waves) copies of 64-row tiles of a [rows, ...] bf16 matrix, D columns
+// from its base, into an AttnTile<D, 64>: copy c of a wave fills the tile rows
+// (4 c + wave) RPC .. + RPC - 1; rows past the end are copies of the last one.
+template <int D>
+struct TileCopy {
+  using T = AttnTile<D, 64>;
+  static constexpr int RPC = 1024 / T::ROW, COPIES = T::COPIES;
+  uint32_t chunk[COPIES];
+  uint32_t lane_row;
+  __device__ __forceinline__ TileCopy(int wave, int lane, size_t row_bytes)
+      : lane_row((uint32_t)(lane / T::CHUNKS) * (uint32_t)row_bytes) {
+#pragma unroll
+    for (int c = 0; c < COPIES; ++c)
+      chunk[c] = (uint32_t)(T::swz((c * 4 + wave) * RPC + lane / T::CHUNKS, lane % T::CHUNKS) * 16);
+  }
+  __device__ __forceinline__ void issue(const unsigned char* g, size_t row_bytes, int row0, int n_rows,
+                                        int wave, int lane, uint32_t lds) const {
+    if (row0 + 64 <= n_rows) {
+      const unsigned char* base = g + (size_t)row0 * row_bytes;
+#pragma unroll
+      for (int c = 0; c < COPIES; ++c)
+        copy_to_lds(base + (size_t)((c * 4 + wave) * RPC) * row_bytes, lane_row + chunk[c],
+                    lds + (c * 4 + wave) * 1024);
+    } else {
+#pragma unroll
+      for (int c = 0; c < COPIES; ++c) {
+        const int r0 = row0 + (c * 4 + wave) * RPC, r0c = min(r0, n_rows - 1);
+        const int rl = min(r0 + lane / T::CHUNKS, n_rows - 1) - r0c;
+        copy_to_lds(g + (size_t)r0c * row_bytes, (uint32_t)(rl * row_bytes) + chunk[c],
+                    lds + (c * 4 + wave) * 1024);
+      }
+    }
+  }
+};
+
+// Which head and query tile a workgroup of a 1-d grid takes. Groups vary fastest, then
+// a group's heads: consecutive workgroups go to different XCDs, so where G is a multiple
+// of 8 the heads that read one group's values share an XCD's L2. The last query tiles
+// (under the causal mask the heaviest) start first.
+struct HeadTile {
+  int h, g, b, qt;
+  __device__ __forceinline__ HeadTile(const ScoredParams& p, int rows) {
+    const int R = p.H / p.G, tiles = (p.N + rows - 1) / rows;
+    g = blockIdx.x % p.G;
+    h = g * R + blockIdx.x / p.G % R;
+    const unsigned rest = blockIdx.x / p.H;
+    b = rest % p.B;
+    qt = tiles - 1 - rest / p.B;
+  }
+};
 
 }  // namespace kl

@@ -21,16 +21,9 @@
 namespace kl {
 namespace {
 
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
-typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) unsigned char lds_u8;
-
 constexpr int kThreads = 256;
 constexpr int kTileRows = 64;  // value rows per tile
 constexpr int kStages = 3;     // tiles in LDS
-constexpr int kSchedMfma = 0x008, kSchedDsRead = 0x100;
 constexpr float kLazy = 8.f;   // the reference moves when a score exceeds it by 2^8
 
 // The online softmax of QB 16-query blocks over NB 16-row blocks of values: sc holds
@@ -124,29 +117,6 @@ __device__ __forceinline__ bool soften(const Form& form, f32x4_t (&sc)[NB][QB], 
   return bad;
 }
 
-__device__ __forceinline__ bf16x8_t finite_or_zero(bf16x8_t v) {
-  u32x4 w = __builtin_bit_cast(u32x4, v);
-#pragma unroll
-  for (int x = 0; x < 4; ++x) w[x] = kl::finite_or_zero(w[x]);
-  return __builtin_bit_cast(bf16x8_t, w);
-}
-
-__device__ __forceinline__ bf16x8_t pack8(f32x4_t a, f32x4_t b) {
-  return __builtin_bit_cast(bf16x8_t, u32x4{pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]),
-                                            pack2(b[2], b[3])});
-}
-
-// Column block db of the value rows of one 32-row step, transposed: rows 4 grp .. + 3
-// and 16 + 4 grp .. + 3 of column 16 db + fr.
-template <int ROW>
-__device__ __forceinline__ bf16x8_t value_columns(int at) {
-  const lds_u8* src = (const lds_u8*)(uintptr_t)(uint32_t)at;
-  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)src);
-  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(src + 16 * ROW));
-  return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
 template <int D, int QB, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p) {
   using T = AttnTile<D, kTileRows>;
@@ -154,14 +124,8 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p)
   constexpr int WQ = 16 * QB, BQ = 4 * WQ, KS = D / 32, DB = D / 16;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   __shared__ int s_any[4][2];
-  // Groups vary fastest, then a group's heads: consecutive workgroups go to different
-  // XCDs, so where G is a multiple of 8 the heads that read one group's values share
-  // an XCD's L2. The last query tiles (under the causal mask the heaviest) start first.
-  const int R = p.H / p.G;
-  const int g = blockIdx.x % p.G, h = g * R + blockIdx.x / p.G % R;
-  const int ntq = (p.N + BQ - 1) / BQ;
-  const long tile_id = blockIdx.x / p.H;
-  const int b = (int)(tile_id % p.B), qt = ntq - 1 - (int)(tile_id / p.B);
+  const HeadTile ht(p, BQ);
+  const int h = ht.h, g = ht.g, b = ht.b, qt = ht.qt;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, grp = lane >> 4;
@@ -196,31 +160,9 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p)
   const size_t row_bytes = (size_t)p.G * D * 2;
   const unsigned char* gV = static_cast<const unsigned char*>(p.v) + ((size_t)b * p.N * p.G + g) * D * 2;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
-  // Copy c of this wave fills tile rows (4 c + wave) RPC .. + RPC - 1.
-  constexpr int RPC = 1024 / T::ROW;
-  uint32_t chunk[T::COPIES];
-#pragma unroll
-  for (int c = 0; c < T::COPIES; ++c)
-    chunk[c] = (uint32_t)(T::swz((c * 4 + wave) * RPC + lane / T::CHUNKS, lane % T::CHUNKS) * 16);
-  const uint32_t lane_row = (uint32_t)(lane / T::CHUNKS) * (uint32_t)row_bytes;
+  const TileCopy<D> cp(wave, lane, row_bytes);
   auto issue = [&](int t, int stage) {
-    const int j0 = (t0 + t) * kTileRows;
-    const uint32_t st = lds0 + stage * T::BYTES;
-    if (j0 + kTileRows <= p.N) {
-      const unsigned char* tb = gV + (size_t)j0 * row_bytes;
-#pragma unroll
-      for (int c = 0; c < T::COPIES; ++c)
-        copy_to_lds(tb + (size_t)((c * 4 + wave) * RPC) * row_bytes, lane_row + chunk[c],
-                    st + (c * 4 + wave) * 1024);
-    } else {
-#pragma unroll
-      for (int c = 0; c < T::COPIES; ++c) {
-        const int r0 = j0 + (c * 4 + wave) * RPC, r0c = min(r0, p.N - 1);
-        const int rl = min(r0 + lane / T::CHUNKS, p.N - 1) - r0c;
-        copy_to_lds(gV + (size_t)r0c * row_bytes, (uint32_t)(rl * row_bytes) + chunk[c],
-                    st + (c * 4 + wave) * 1024);
-      }
-    }
+    cp.issue(gV, row_bytes, (t0 + t) * kTileRows, p.N, wave, lane, lds0 + stage * T::BYTES);
   };
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s)
@@ -266,10 +208,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p)
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) offS[ks] = fi.s(ks);
       bf16x8_t sa[2][KS];
-      auto rows = [&](int kb, int ks) {
-        return *(const __attribute__((address_space(3))) bf16x8_t*)(uintptr_t)(
-            uint32_t)(offS[ks] + kb * 16 * T::ROW);
-      };
+      auto rows = [&](int kb, int ks) { return lds_rows(offS[ks] + kb * 16 * T::ROW); };
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) sa[0][ks] = rows(0, ks);
 #pragma unroll
@@ -304,7 +243,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p)
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) pf[qb] = pack8(sc[2 * ks][qb], sc[2 * ks + 1][qb]);
 #pragma unroll
-      for (int db = 0; db < DB; ++db) av[db] = value_columns<T::ROW>(offT[db] + ks * 32 * T::ROW);
+      for (int db = 0; db < DB; ++db) av[db] = lds_columns<T::ROW>(offT[db] + ks * 32 * T::ROW);
       if (bad) {
 #pragma unroll
         for (int db = 0; db < DB; ++db) av[db] = finite_or_zero(av[db]);
@@ -327,6 +266,20 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p)
     if (q >= p.N) continue;
     const bool none = seen[qb].lo >= seen[qb].hi;
     const float inv = none ? 0.f : 1.f / sum;
+    if (p.Dd) {  // for the backward: rowsum(dO * O), O in fp32, in place of the output
+      const uint16_t* go = static_cast<const uint16_t*>(p.dout) + (((size_t)b * p.N + q) * p.H + h) * D + grp * 4;
+      float d0 = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(go + db * 16);
+        d0 = fmaf(bf16_lo(w[0]), o[db][qb][0], fmaf(bf16_hi(w[0]), o[db][qb][1], d0));
+        d0 = fmaf(bf16_lo(w[1]), o[db][qb][2], fmaf(bf16_hi(w[1]), o[db][qb][3], d0));
+      }
+      d0 += __shfl_xor(d0, 16);
+      d0 += __shfl_xor(d0, 32);
+      if (grp == 0) p.Dd[((size_t)b * p.H + h) * p.N + q] = none ? 0.f : d0 * inv;
+      continue;
+    }
     if (p.lse && grp == 0)
       p.lse[((size_t)b * p.H + h) * p.N + q] = none ? -INFINITY : (m[qb] + __log2f(sum)) * kScoredLn2;
     const size_t at = (((size_t)b * p.N + q) * p.H + h) * D + grp * 4;

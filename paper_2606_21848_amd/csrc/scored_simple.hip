@@ -255,6 +255,7 @@ hipError_t launch_scored_forward(const ScoredParams& p, hipStream_t stream) {
 }
 
 hipError_t launch_scored_backward(const ScoredParams& p, hipStream_t stream) {
+  if (p.dtype == KL_BF16) return launch_scored_backward_bf16(p, stream);
   const unsigned tiles = (unsigned)p.B * ((p.N + kRows - 1) / kRows);
   return pick(p.dtype, p.D, [&](auto t, auto d) {
     hipLaunchKernelGGL((dq_kernel<decltype(t), decltype(d)::value>), dim3(p.H * tiles), dim3(256), 0,
