@@ -1381,10 +1381,33 @@ int keyless_scored_backward(const void* q_routed, const void* v, const void* out
   return hip_status(kl::launch_scored_backward(p, static_cast<hipStream_t>(stream)), who);
 }
 
+namespace {
+
+// Work split of a drafted-token decode, from the shapes alone (the kernels share the
+// rows out from the lengths): about two workgroups per CU, chunks of at least 128 rows;
+// a capacity of at most 1024 rows is one chunk, without partial results or a merge.
+struct TreePlan {
+  int chunks, least;
+  size_t ml, total;
+};
+TreePlan plan_tree(const kl_value_cache* c, int B, int T, int H) {
+  TreePlan pl{1, 1 << 30, 0, 0};
+  if (c->dtype != KL_BF16 || cache_capacity(c) <= 1024) return pl;
+  const long M = (long)T * (H / c->G), blocks = (M + 31) / 32;
+  pl.chunks = (int)std::max(1L, kBalancedWorkgroups / (c->G * blocks));
+  pl.least = 4;
+  const size_t rows = (size_t)(pl.chunks + B) * c->G * M;
+  pl.ml = align256(rows * c->d_head * sizeof(float));
+  pl.total = pl.ml + align256(rows * 2 * sizeof(float));
+  return pl;
+}
+
+}  // namespace
+
 size_t keyless_tree_decode_workspace_size(const kl_value_cache* cache, int B, int T, int H) {
   if (!cache || B <= 0 || T <= 0 || T > kl::kMaxDrafts || H <= 0 || cache->G <= 0 || H % cache->G != 0)
     return 0;
-  return 0;
+  return plan_tree(cache, B, T, H).total;
 }
 
 int keyless_tree_decode(const void* q_routed, const kl_value_cache* cache,
@@ -1440,6 +1463,13 @@ int keyless_tree_decode(const void* q_routed, const kl_value_cache* cache,
   p.max_blocks = cache->max_blocks_per_seq;
   p.scale = scale_or_default(scale, p.D);
   p.cap = cap;
+  const TreePlan pl = plan_tree(cache, B, T, H);
+  p.chunks = pl.chunks;
+  p.least = pl.least;
+  if (need) {
+    p.part = static_cast<float*>(ws);
+    p.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.ml);
+  }
   return hip_status(kl::launch_tree_decode(p, static_cast<hipStream_t>(stream)), who);
 }
 

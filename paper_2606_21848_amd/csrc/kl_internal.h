@@ -308,8 +308,14 @@ struct TreeParams {
   bool paged;
   int L_max, block_shift, num_blocks, max_blocks;
   float scale, cap;
+  // Work split: at most chunks + B chunks of at least `least` 32-row tiles each, and
+  // the partial results of those of split sequences (null: every sequence is one chunk).
+  int chunks, least;
+  float* part;     // [chunks + B, G, T H / G, D]
+  float* part_ml;  // [chunks + B, G, T H / G, 2]
 };
 hipError_t launch_tree_decode(const TreeParams& p, hipStream_t stream);
+hipError_t launch_tree_decode_bf16(const TreeParams& p, hipStream_t stream);
 
 // Rows n + path[b, k] to rows n + k for k < kept[b], n = lengths_before[b].
 struct KeepParams {

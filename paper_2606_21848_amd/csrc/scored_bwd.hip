@@ -40,17 +40,17 @@ __device__ __forceinline__ void copy_dword_to_lds(const void* gbase, uint32_t vo
 // P and dz (times `scale4` / 4 where it is not 1) of one pair: `k` the key, `dp` dP - Dd.
 // shift = C - lse in log2 units.
 template <class Form, bool CAP, bool BIAS>
-__device__ __forceinline__ void weigh(const Form& form, float s, float dist, float dp, float shift,
-                                      float scale, float& w, float& dz) {
+__device__ __forceinline__ void weigh(const Form& form, float s, float slope, float dist, float dp,
+                                      float shift, float scale, float& w, float& dz) {
   if constexpr (CAP) {
     const float k = form.bent(s);
     float x = k;
-    if constexpr (BIAS) x = fmaf(-form.slope2, fabsf(dist), fmaf(k, -2.f * form.cap2, form.cap2));
+    if constexpr (BIAS) x = fmaf(-slope, fabsf(dist), fmaf(k, -2.f * form.cap2, form.cap2));
     w = fast_exp2(form.shifted(x, shift));
     const float k4 = k * (4.f * scale);
     dz = w * dp * fmaf(-k4, k, k4);  // 1 - tanh^2 = 4 k (1 - k)
   } else {
-    w = fast_exp2(form.shifted(form.key(s, dist), shift));
+    w = fast_exp2(form.shifted(form.key(s, [&](float x) { return fmaf(-slope, fabsf(dist), x); }), shift));
     dz = w * dp * scale;
   }
 }
@@ -130,7 +130,8 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) 
   bf16x8_t qf[QB][KS], df[QB][KS];
   f32x4_t ndd[QB], acc[DB][QB];
   float shift[QB];
-  const Form form(p.scale, p.cap, BIAS ? p.slopes[h] : 0.f);
+  const Form form(p.scale, p.cap);
+  const float slope = BIAS ? p.slopes[h] * kScoredLog2e : 0.f;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     const int q = q0 + qb * 16 + fr, qq = min(q, p.N - 1);
@@ -210,7 +211,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) 
       const int jl = j0 + 32 * ks + grp * 4;
       auto unseen = [&](int qb, int hh, int r) {
         const int j = jl + hh * 16 + r;
-        return j < seen[qb].lo || j >= seen[qb].hi;
+        return (j < seen[qb].lo) | (j >= seen[qb].hi);
       };
       bool bad = false;  // see the forward: values that a query must not see are not finite
       if (edge) {
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) 
           for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              bad |= unseen(qb, hh, r) && (not_finite(sc[hh][qb][r]) || not_finite(dp[hh][qb][r]));
+              bad |= unseen(qb, hh, r) & (not_finite(sc[hh][qb][r]) | not_finite(dp[hh][qb][r]));
         bad = __builtin_amdgcn_ballot_w64(bad) != 0;
         if (bad) {
 #pragma unroll
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) 
             for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
               for (int r = 0; r < 4; ++r)
-                if (not_finite(sc[hh][qb][r])) dp[hh][qb][r] = __builtin_nanf("");
+                dp[hh][qb][r] = not_finite(sc[hh][qb][r]) ? __builtin_nanf("") : dp[hh][qb][r];
         }
       }
       bf16x8_t pf[QB];
@@ -241,7 +242,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) 
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             float w, dz;
-            weigh<Form, CAP, BIAS>(form, sc[hh][qb][r], dist - (float)(hh * 16 + r), dp[hh][qb][r],
+            weigh<Form, CAP, BIAS>(form, sc[hh][qb][r], slope, dist - (float)(hh * 16 + r), dp[hh][qb][r],
                                    shift[qb], 1.f, w, dz);
             sc[hh][qb][r] = dz;
           }
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) 
           for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              if (unseen(qb, hh, r)) sc[hh][qb][r] = 0.f;
+              sc[hh][qb][r] = unseen(qb, hh, r) ? 0.f : sc[hh][qb][r];
       }
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) pf[qb] = pack8(sc[0][qb], sc[1][qb]);
@@ -396,7 +397,8 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
     if (s.x >= kv0 + 16 * KVB || s.y <= kv0) continue;  // no row of the tile sees this wave's
     // Rows past the end see nothing, so that a tile with a tail is an edge.
     const bool edge = s.z > kv0 || s.w < kv0 + 16 * KVB;
-    const Form form(p.scale, p.cap, BIAS ? p.slopes[h] : 0.f);
+    const Form form(p.scale, p.cap);
+    const float slope = BIAS ? p.slopes[h] * kScoredLog2e : 0.f;
 #pragma unroll
     for (int qs = 0; qs < 2; ++qs) {
       u32x4 wp[KVB], wz[KVB];
@@ -451,7 +453,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const int kv = kv0 + kb * 16 + fr;
-              odd |= (kv < lo[r] || kv >= hi[r]) && (not_finite(sc[kb][r]) || not_finite(dp[kb][r]));
+              odd |= ((kv < lo[r]) | (kv >= hi[r])) & (not_finite(sc[kb][r]) | not_finite(dp[kb][r]));
             }
           odd = __builtin_amdgcn_ballot_w64(odd) != 0;
           bad |= odd;
@@ -460,7 +462,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
             for (int kb = 0; kb < KVB; ++kb)
 #pragma unroll
               for (int r = 0; r < 4; ++r)
-                if (not_finite(sc[kb][r]) || not_finite(dp[kb][r])) sc[kb][r] = __builtin_nanf("");
+                sc[kb][r] = not_finite(sc[kb][r]) | not_finite(dp[kb][r]) ? __builtin_nanf("") : sc[kb][r];
           }
         }
 #pragma unroll
@@ -469,14 +471,16 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
           float w[4], dz[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            weigh<Form, CAP, BIAS>(form, sc[kb][r], dist + (float)r, dp[kb][r] - dd[r],
+            weigh<Form, CAP, BIAS>(form, sc[kb][r], slope, dist + (float)r, dp[kb][r] - dd[r],
                                    fmaf(-lse[r], kScoredLog2e, form.C()), p.scale, w[r], dz[r]);
           }
           if (edge) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const int kv = kv0 + kb * 16 + fr;
-              if (kv < lo[r] || kv >= hi[r]) w[r] = dz[r] = 0.f;
+              const bool unseen = (kv < lo[r]) | (kv >= hi[r]);
+              w[r] = unseen ? 0.f : w[r];
+              dz[r] = unseen ? 0.f : dz[r];
             }
           }
           wp[kb][2 * hh] = pack2(w[0], w[1]);

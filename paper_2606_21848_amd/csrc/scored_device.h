@@ -70,10 +70,9 @@ struct ScoreForm {
   static constexpr bool kFalling = CAP && !BIAS;  // a larger k is a smaller score
   float scale2;       // scale log2 e
   float cap2, twice;  // cap log2 e; 2 scale log2 e / cap
-  float slope2;       // slope log2 e
-  __device__ __forceinline__ ScoreForm(float scale, float cap, float slope)
+  __device__ __forceinline__ ScoreForm(float scale, float cap)
       : scale2(scale * kScoredLog2e), cap2(cap * kScoredLog2e),
-        twice(CAP ? 2.f * scale * kScoredLog2e / cap : 0.f), slope2(slope * kScoredLog2e) {}
+        twice(CAP ? 2.f * scale * kScoredLog2e / cap : 0.f) {}
   __device__ __forceinline__ float A() const { return BIAS ? 1.f : CAP ? -2.f * cap2 : scale2; }
   __device__ __forceinline__ float C() const { return CAP && !BIAS ? cap2 : 0.f; }
   static __device__ __forceinline__ float unseen() { return kFalling ? INFINITY : -INFINITY; }
@@ -81,13 +80,12 @@ struct ScoreForm {
   __device__ __forceinline__ float bent(float s) const {
     return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * twice));
   }
-  __device__ __forceinline__ float key(float s, float dist) const {
+  // The key of a dot product; bias(x) gives x with its bias taken off, in log2 units.
+  template <class Bias>
+  __device__ __forceinline__ float key(float s, Bias bias) const {
     float k = s;
     if constexpr (CAP) k = bent(s);
-    if constexpr (BIAS) {
-      k = CAP ? fmaf(k, -2.f * cap2, cap2) : k * scale2;
-      k = fmaf(-slope2, fabsf(dist), k);
-    }
+    if constexpr (BIAS) k = bias(CAP ? fmaf(k, -2.f * cap2, cap2) : k * scale2);
     return k;
   }
   // The better of two keys.
@@ -198,5 +196,90 @@ struct HeadTile {
     qt = tiles - 1 - rest / p.B;
   }
 };
+
+constexpr float kLazy = 8.f;  // a softmax reference moves when a score exceeds it by 2^8
+
+// The online softmax of QB 16-query blocks over NB 16-row blocks of values: sc holds
+// the dot products on entry (lane: query fr of block qb, rows 16 kb + 4 grp + r of the
+// tile) and the weights on return. `edge` (uniform): some row is not seen by some query,
+// as unseen(qb, kb, r) tells; bias(x, qb, kb, r) takes a pair's bias off; returns whether a pair that is not seen has a product that
+// is not finite (uniform). Its value row is then not finite, and 0 times it would not be
+// either: the caller takes the values that are not finite as zeros, and a query that
+// sees such a product gets NaN as its score here, and with it as its result.
+template <int D, int NB, int QB, class Form, class Unseen, class Bias>
+__device__ __forceinline__ bool soften(const Form& form, f32x4_t (&sc)[NB][QB], f32x4_t (&o)[D / 16][QB],
+                                       float (&m)[QB], float (&l)[QB], bool edge, Unseen unseen, Bias bias) {
+  bool bad = false;
+  if (edge) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          bad |= unseen(qb, kb, r) & not_finite(sc[kb][qb][r]);
+    bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+    if (bad) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            sc[kb][qb][r] = not_finite(sc[kb][qb][r]) ? __builtin_nanf("") : sc[kb][qb][r];
+    }
+  }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sc[kb][qb][r] = form.key(sc[kb][qb][r], [&](float x) { return bias(x, qb, kb, r); });
+  if (edge) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          sc[kb][qb][r] = unseen(qb, kb, r) ? Form::unseen() : sc[kb][qb][r];
+  }
+  float top[QB];  // this lane's best score per query
+  bool grow = false;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    float k = sc[0][qb][0];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) k = Form::best(k, sc[kb][qb][r]);
+    top[qb] = fmaf(form.A(), k, form.C());
+    grow |= top[qb] > m[qb] + kLazy;
+  }
+  if (__builtin_amdgcn_ballot_w64(grow)) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      float t = fmaxf(top[qb], __shfl_xor(top[qb], 16));
+      t = fmaxf(t, __shfl_xor(t, 32));
+      const float mn = t > m[qb] + kLazy ? t : m[qb];
+      const float alpha = m[qb] == -INFINITY ? 0.f : fast_exp2(m[qb] - mn);
+      l[qb] *= alpha;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) o[i][qb] *= alpha;
+      m[qb] = mn;
+    }
+  }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const float shift = form.C() - (m[qb] == -INFINITY ? 0.f : m[qb]);
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sc[kb][qb][r] = fast_exp2(form.shifted(sc[kb][qb][r], shift));
+      l[qb] += (sc[kb][qb][0] + sc[kb][qb][1]) + (sc[kb][qb][2] + sc[kb][qb][3]);
+    }
+  }
+  return bad;
+}
 
 }  // namespace kl

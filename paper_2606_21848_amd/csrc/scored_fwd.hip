@@ -24,99 +24,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTileRows = 64;  // value rows per tile
 constexpr int kStages = 3;     // tiles in LDS
-constexpr float kLazy = 8.f;   // the reference moves when a score exceeds it by 2^8
-
-// The online softmax of QB 16-query blocks over NB 16-row blocks of values: sc holds
-// the dot products on entry (lane: query fr of block qb, rows 16 kb + 4 grp + r of the
-// tile from row j0) and the weights on return. `edge` (uniform): some row is not seen
-// by some query; returns whether a pair that is not seen has a product that is not
-// finite (uniform). Its value row is then not finite, and 0 times it would not be
-// either: the caller takes the values that are not finite as zeros, and a query that
-// sees such a product gets NaN as its score here, and with it as its result.
-template <int D, int NB, int QB, class Form>
-__device__ __forceinline__ bool soften(const Form& form, f32x4_t (&sc)[NB][QB], f32x4_t (&o)[D / 16][QB],
-                                       float (&m)[QB], float (&l)[QB], const SeenRange (&seen)[QB],
-                                       int j0, int q0, int fr, int grp, bool edge) {
-  bool bad = false;
-  if (edge) {
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-      for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int j = j0 + kb * 16 + grp * 4 + r;
-          const bool out = j < seen[qb].lo || j >= seen[qb].hi;
-          bad |= out && not_finite(sc[kb][qb][r]);
-        }
-    bad = __builtin_amdgcn_ballot_w64(bad) != 0;
-    if (bad) {
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-        for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (not_finite(sc[kb][qb][r])) sc[kb][qb][r] = __builtin_nanf("");
-    }
-  }
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const float d0 = (float)(q0 + qb * 16 + fr - j0 - grp * 4);
-#pragma unroll
-    for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sc[kb][qb][r] = form.key(sc[kb][qb][r], d0 - (float)(kb * 16 + r));
-  }
-  if (edge) {
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-      for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int j = j0 + kb * 16 + grp * 4 + r;
-          if (j < seen[qb].lo || j >= seen[qb].hi) sc[kb][qb][r] = Form::unseen();
-        }
-  }
-  float top[QB];  // this lane's best score per query
-  bool grow = false;
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    float k = sc[0][qb][0];
-#pragma unroll
-    for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) k = Form::best(k, sc[kb][qb][r]);
-    top[qb] = fmaf(form.A(), k, form.C());
-    grow |= top[qb] > m[qb] + kLazy;
-  }
-  if (__builtin_amdgcn_ballot_w64(grow)) {
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      float t = fmaxf(top[qb], __shfl_xor(top[qb], 16));
-      t = fmaxf(t, __shfl_xor(t, 32));
-      const float mn = t > m[qb] + kLazy ? t : m[qb];
-      const float alpha = m[qb] == -INFINITY ? 0.f : fast_exp2(m[qb] - mn);
-      l[qb] *= alpha;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) o[i][qb] *= alpha;
-      m[qb] = mn;
-    }
-  }
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const float shift = form.C() - (m[qb] == -INFINITY ? 0.f : m[qb]);
-#pragma unroll
-    for (int kb = 0; kb < NB; ++kb) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sc[kb][qb][r] = fast_exp2(form.shifted(sc[kb][qb][r], shift));
-      l[qb] += (sc[kb][qb][0] + sc[kb][qb][1]) + (sc[kb][qb][2] + sc[kb][qb][3]);
-    }
-  }
-  return bad;
-}
-
 template <int D, int QB, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p) {
   using T = AttnTile<D, kTileRows>;
@@ -177,7 +84,8 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p)
     for (int ks = 0; ks < KS; ++ks)
       qf[qb][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(src + ks * 32));
   }
-  const Form form(p.scale, p.cap, BIAS ? p.slopes[h] : 0.f);
+  const Form form(p.scale, p.cap);
+  const float slope = BIAS ? p.slopes[h] * kScoredLog2e : 0.f;
   f32x4_t o[DB][QB];
   float m[QB], l[QB];
 #pragma unroll
@@ -233,7 +141,16 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p)
       __builtin_amdgcn_sched_group_barrier(kSchedMfma, KS * QB, 0);
     }
     const bool edge = j0 < sb.all_lo || j0 + kTileRows > sb.all_hi;
-    const bool bad = soften<D, 4, QB>(form, sc, o, m, l, seen, j0, q0, fr, grp, edge);
+    const int jl = j0 + grp * 4;
+    const bool bad = soften<D, 4, QB>(
+        form, sc, o, m, l, edge,
+        [&](int qb, int kb, int r) {
+          const int j = jl + kb * 16 + r;
+          return (j < seen[qb].lo) | (j >= seen[qb].hi);
+        },
+        [&](float x, int qb, int kb, int r) {
+          return fmaf(-slope, fabsf((float)(q0 + qb * 16 + fr - jl) - (float)(kb * 16 + r)), x);
+        });
     int offT[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) offT[db] = fi.t(db);

@@ -266,6 +266,7 @@ hipError_t launch_scored_backward(const ScoredParams& p, hipStream_t stream) {
 }
 
 hipError_t launch_tree_decode(const TreeParams& p, hipStream_t stream) {
+  if (p.dtype == KL_BF16) return launch_tree_decode_bf16(p, stream);
   return pick(p.dtype, p.D, [&](auto t, auto d) {
     hipLaunchKernelGGL((tree_kernel<decltype(t), decltype(d)::value>), dim3(p.H * p.T * p.B),
                        dim3(256), 0, stream, p);

@@ -297,7 +297,8 @@ def test_on_another_stream_and_in_a_graph(lib, dtype):
         ws.fill_(0xFF)
         graph.replay()
         torch.cuda.synchronize()
-        assert all(torch.equal(a, b) for a, b in zip(bufs, (out, lse, dq, dv))), f"replay {rep}"
+        same = [bool(torch.equal(a, b)) for a, b in zip(bufs, (out, lse, dq, dv))]
+        assert all(same), f"replay {rep}"
 
 
 def test_a_long_sequence_by_rows(lib):

@@ -307,7 +307,7 @@ def test_draft_step_graph_replays(lib, dtype):
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
             step()
-        graphs.append((g, vc, out))
+        graphs.append((g, vc, out, ws))  # a captured workspace has to live as long as its graph
     for rep in range(3):
         q.copy_(synth.normal((B, T, H, d), 420 + rep, 1, 1.0, dtype))
         rows.copy_(synth.normal((B, T, G, d), 420 + rep, 2, 1.0, dtype))
@@ -315,7 +315,7 @@ def test_draft_step_graph_replays(lib, dtype):
         kb.value_cache_append(ref, rows, n)
         want = kb.keyless_tree_decode(q, ref, n, words, cap=25.0, slopes=sl)
         kb.value_cache_keep(ref, n, path, kept)
-        for _, vc, _ in graphs:
+        for _, vc, _, _ in graphs:
             vc.data.copy_(base)
         torch.cuda.synchronize()
         side = torch.cuda.Stream()
@@ -323,5 +323,6 @@ def test_draft_step_graph_replays(lib, dtype):
             graphs[1][0].replay()
         graphs[0][0].replay()
         torch.cuda.synchronize()
-        for g, vc, out in graphs:
-            assert torch.equal(out, want) and torch.equal(vc.data, ref.data), f"replay {rep}"
+        for g, vc, out, _ in graphs:
+            same = bool(torch.equal(out, want)), bool(torch.equal(vc.data, ref.data))
+            assert same == (True, True), f"replay {rep}"
