@@ -1282,8 +1282,8 @@ int check_scored_args(const char* who, const void* q, const void* v, const void*
   return KL_OK;
 }
 
-// Workspace of keyless_scored_backward: the row sums, and for bf16 what each row and
-// each 64-row tile sees and the fp32 partial sums of dv over S splits.
+// Workspace of keyless_scored_backward: the row sums, what each row and each query tile
+// (64 rows, fp32 16) sees, and for bf16 the fp32 partial sums of dv over S splits.
 struct ScoredBwdLayout {
   size_t lo, hi, tiles, part, total;
   int S;
@@ -1291,12 +1291,12 @@ struct ScoredBwdLayout {
 ScoredBwdLayout scored_bwd_layout(int B, int N, int H, int G, int d_head, kl_dtype dtype) {
   ScoredBwdLayout L{};
   L.S = 1;
-  L.lo = L.total = bwd_rows_bytes(B, N, H);
-  if (dtype != KL_BF16) return L;
-  L.S = kl::attn_bwd_splits(B, N, H, G, true);
+  const long tile = dtype == KL_BF16 ? 64 : 16;
+  if (dtype == KL_BF16) L.S = kl::attn_bwd_splits(B, N, H, G, true);
+  L.lo = bwd_rows_bytes(B, N, H);
   L.hi = L.lo + align256((size_t)B * N * sizeof(int));
   L.tiles = L.hi + align256((size_t)B * N * sizeof(int));
-  L.part = L.tiles + align256((size_t)B * ((N + 63) / 64) * 4 * sizeof(int));
+  L.part = L.tiles + align256((size_t)B * ((N + tile - 1) / tile) * 4 * sizeof(int));
   L.total = L.part + (L.S > 1 ? align256((size_t)L.S * B * N * G * d_head * sizeof(float)) : 0);
   return L;
 }
@@ -1336,7 +1336,8 @@ int keyless_scored_forward(const void* q_routed, const void* v, const kl_scoring
   p.out = out;
   p.lse = lse;
   p.out_f32 = out_f32;
-  return hip_status(kl::launch_scored_forward(p, static_cast<hipStream_t>(stream)), who);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return hip_status(p.dtype == KL_BF16 ? kl::launch_scored_forward_bf16(p, st) : kl::launch_scored_forward_f32(p, st), who);
 }
 
 size_t keyless_scored_backward_workspace_size(int B, int N, int H, int G, int d_head,
@@ -1378,7 +1379,8 @@ int keyless_scored_backward(const void* q_routed, const void* v, const void* out
   p.part = reinterpret_cast<float*>(w + L.part);
   p.dq = dq_routed;
   p.dv = dv;
-  return hip_status(kl::launch_scored_backward(p, static_cast<hipStream_t>(stream)), who);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return hip_status(p.dtype == KL_BF16 ? kl::launch_scored_backward_bf16(p, st) : kl::launch_scored_backward_f32(p, st), who);
 }
 
 namespace {
@@ -1392,8 +1394,9 @@ struct TreePlan {
 };
 TreePlan plan_tree(const kl_value_cache* c, int B, int T, int H) {
   TreePlan pl{1, 1 << 30, 0, 0};
-  if (c->dtype != KL_BF16 || cache_capacity(c) <= 1024) return pl;
-  const long M = (long)T * (H / c->G), blocks = (M + 31) / 32;
+  if (cache_capacity(c) <= 1024) return pl;
+  const long M = (long)T * (H / c->G), rows_per = c->dtype == KL_BF16 ? 32 : 16;
+  const long blocks = (M + rows_per - 1) / rows_per;
   pl.chunks = (int)std::max(1L, kBalancedWorkgroups / (c->G * blocks));
   pl.least = 4;
   const size_t rows = (size_t)(pl.chunks + B) * c->G * M;
@@ -1470,7 +1473,8 @@ int keyless_tree_decode(const void* q_routed, const kl_value_cache* cache,
     p.part = static_cast<float*>(ws);
     p.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.ml);
   }
-  return hip_status(kl::launch_tree_decode(p, static_cast<hipStream_t>(stream)), who);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return hip_status(p.dtype == KL_BF16 ? kl::launch_tree_decode_bf16(p, st) : kl::launch_tree_decode_f32(p, st), who);
 }
 
 int value_cache_keep(const kl_value_cache* cache, const int32_t* lengths_before,

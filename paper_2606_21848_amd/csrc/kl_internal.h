@@ -279,16 +279,17 @@ struct ScoredParams {
   float* Dd;             // [B, H, N] scratch: rowsum(P * dP)
   void* dq;
   void* dv;
-  int* row_lo;           // [B, N] scratch: what each query row sees (bf16)
+  int* row_lo;           // [B, N] scratch: what each query row sees
   int* row_hi;
-  void* tile_sees;       // [B, ceil(N / 64), 4] int scratch: rows seen by any, by all rows of a tile (bf16)
+  void* tile_sees;       // [B, tiles, 4] int scratch: the rows seen by any and by all rows of a query
+                         // tile (bf16: 64 rows, fp32: 16)
   int S;                 // splits of the dV sums, 1 for none (bf16)
   float* part;           // their fp32 partial sums [S, B, N, G, D]
 };
-hipError_t launch_scored_forward(const ScoredParams& p, hipStream_t stream);
 hipError_t launch_scored_forward_bf16(const ScoredParams& p, hipStream_t stream);
-hipError_t launch_scored_backward(const ScoredParams& p, hipStream_t stream);
+hipError_t launch_scored_forward_f32(const ScoredParams& p, hipStream_t stream);
 hipError_t launch_scored_backward_bf16(const ScoredParams& p, hipStream_t stream);
+hipError_t launch_scored_backward_f32(const ScoredParams& p, hipStream_t stream);
 
 // Most drafted tokens per sequence: a token's row of the tree is one 64-bit word.
 constexpr int kMaxDrafts = 64;
@@ -314,8 +315,9 @@ struct TreeParams {
   float* part;     // [chunks + B, G, T H / G, D]
   float* part_ml;  // [chunks + B, G, T H / G, 2]
 };
-hipError_t launch_tree_decode(const TreeParams& p, hipStream_t stream);
 hipError_t launch_tree_decode_bf16(const TreeParams& p, hipStream_t stream);
+hipError_t launch_tree_decode_f32(const TreeParams& p, hipStream_t stream);
+hipError_t launch_tree_merge(const TreeParams& p, hipStream_t stream);
 
 // Rows n + path[b, k] to rows n + k for k < kept[b], n = lengths_before[b].
 struct KeepParams {

@@ -371,11 +371,15 @@ hipError_t launch_merge(const TreeParams& p, hipStream_t st) {
 template <int D>
 hipError_t launch_d(const TreeParams& p, hipStream_t st) {
   const hipError_t e = p.T * (p.H / p.G) <= 16 ? launch_qb<D, 1>(p, st) : launch_qb<D, 2>(p, st);
-  if (e != hipSuccess || !p.part) return e;
-  return launch_merge<uint16_t, D>(p, st);
+  return e != hipSuccess || !p.part ? e : launch_tree_merge(p, st);
 }
 
 }  // namespace
+
+hipError_t launch_tree_merge(const TreeParams& p, hipStream_t st) {
+  if (p.dtype == KL_BF16) return p.D == 128 ? launch_merge<uint16_t, 128>(p, st) : launch_merge<uint16_t, 64>(p, st);
+  return p.D == 128 ? launch_merge<float, 128>(p, st) : launch_merge<float, 64>(p, st);
+}
 
 hipError_t launch_tree_decode_bf16(const TreeParams& p, hipStream_t st) {
   return p.D == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);
