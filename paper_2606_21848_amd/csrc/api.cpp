@@ -1282,21 +1282,22 @@ int check_scored_args(const char* who, const void* q, const void* v, const void*
   return KL_OK;
 }
 
-// Workspace of keyless_scored_backward: the row sums, what each row and each query tile
-// (64 rows, fp32 16) sees, and for bf16 the fp32 partial sums of dv over S splits.
+// Workspace of keyless_scored_backward: the row sums, what each row and each query block
+// (32 rows, fp32 16) sees, and for bf16 the fp32 partial sums of dv over S splits.
 struct ScoredBwdLayout {
-  size_t lo, hi, tiles, part, total;
+  size_t lo, hi, tiles, splits, part, total;
   int S;
 };
 ScoredBwdLayout scored_bwd_layout(int B, int N, int H, int G, int d_head, kl_dtype dtype) {
   ScoredBwdLayout L{};
   L.S = 1;
-  const long tile = dtype == KL_BF16 ? 64 : 16;
+  const long tile = dtype == KL_BF16 ? 32 : 16;
   if (dtype == KL_BF16) L.S = kl::attn_bwd_splits(B, N, H, G, true);
   L.lo = bwd_rows_bytes(B, N, H);
   L.hi = L.lo + align256((size_t)B * N * sizeof(int));
   L.tiles = L.hi + align256((size_t)B * N * sizeof(int));
-  L.part = L.tiles + align256((size_t)B * ((N + tile - 1) / tile) * 4 * sizeof(int));
+  L.splits = L.tiles + align256((size_t)B * ((N + tile - 1) / tile) * 4 * sizeof(int));
+  L.part = L.splits + align256((size_t)B * ((N + 191) / 192) * sizeof(int));
   L.total = L.part + (L.S > 1 ? align256((size_t)L.S * B * N * G * d_head * sizeof(float)) : 0);
   return L;
 }
@@ -1376,6 +1377,7 @@ int keyless_scored_backward(const void* q_routed, const void* v, const void* out
   p.row_hi = reinterpret_cast<int*>(w + L.hi);
   p.tile_sees = w + L.tiles;
   p.S = L.S;
+  p.tile_splits = reinterpret_cast<int*>(w + L.splits);
   p.part = reinterpret_cast<float*>(w + L.part);
   p.dq = dq_routed;
   p.dv = dv;

@@ -282,10 +282,12 @@ struct ScoredParams {
   int* row_lo;           // [B, N] scratch: what each query row sees
   int* row_hi;
   void* tile_sees;       // [B, tiles, 4] int scratch: the rows seen by any and by all rows of a query
-                         // tile (bf16: 64 rows, fp32: 16)
-  int S;                 // splits of the dV sums, 1 for none (bf16)
+                         // block (bf16: 32 rows, fp32: 16)
+  int S;                 // most splits of the dV sums, 1 for none (bf16)
+  int* tile_splits;      // [ceil(N / 192), B] scratch: the splits of each value tile
   float* part;           // their fp32 partial sums [S, B, N, G, D]
 };
+bool scored_few_query_tiles(const ScoredParams& p);
 hipError_t launch_scored_forward_bf16(const ScoredParams& p, hipStream_t stream);
 hipError_t launch_scored_forward_f32(const ScoredParams& p, hipStream_t stream);
 hipError_t launch_scored_backward_bf16(const ScoredParams& p, hipStream_t stream);

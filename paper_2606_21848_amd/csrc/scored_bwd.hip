@@ -27,6 +27,7 @@ constexpr int kThreads = 256;
 constexpr int kTileRows = 64;
 constexpr int kStages = 3;           // value tiles in LDS (dQ~)
 constexpr int QB = 2, BQ = 64 * QB;  // 16-row query blocks per wave, query rows per workgroup (dQ~)
+constexpr int kLeastItems = 4;       // (head, query tile) pairs of a split of the dV sums
 constexpr int KVB = 3, BKV = 64 * KVB;  // value blocks per wave, value rows per workgroup (dV)
 
 // One 4-byte-per-lane copy from global memory straight into LDS.
@@ -55,23 +56,11 @@ __device__ __forceinline__ void weigh(const Form& form, float s, float slope, fl
   }
 }
 
-template <int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) {
-  using T = AttnTile<D, kTileRows>;
-  using Form = ScoreForm<CAP, BIAS>;
-  constexpr int KS = D / 32, DB = D / 16;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  __shared__ int s_sees[4][4];
-  const HeadTile ht(p, BQ);
-  const int h = ht.h, g = ht.g, b = ht.b, qt = ht.qt;
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int fr = lane & 15, grp = lane >> 4;
-  const int q0 = qt * BQ + wave * 16 * QB;
-
-  // What the rows see; the first head's workgroup publishes it (rows past the end see
-  // nothing there, so that a query tile with a tail counts as seen in part).
-  SeenRange seen[QB];
+// What the 32 query rows from q0 on see (lane: rows q0 + 16 qb + fr), into `seen` and the
+// bounds returned; `publish`: for the dV kernel too (rows past the end see nothing there, so
+// that a block with a tail counts as seen in part).
+__device__ __forceinline__ SeenBounds seen_by_rows(const ScoredParams& p, int b, int q0, int fr, int grp,
+                                                   bool publish, SeenRange (&seen)[QB]) {
   SeenBounds sb, pub;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
@@ -79,30 +68,181 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) 
     seen[qb] = seen_range(p, b, min(q, p.N - 1));
     sb.add(seen[qb]);
     pub.add(q < p.N ? seen[qb] : SeenRange{0, 0});
-    if (h == 0 && grp == 0 && q < p.N) {
+    if (publish && grp == 0 && q < p.N) {
       p.row_lo[(size_t)b * p.N + q] = seen[qb].lo;
       p.row_hi[(size_t)b * p.N + q] = seen[qb].hi;
     }
   }
   sb.over_lanes(15);
-  pub.over_lanes(15);
   sb.make_uniform();
+  if (publish && q0 < p.N) {
+    pub.over_lanes(15);
+    if (fr == 0 && grp == 0)
+      static_cast<i32x4*>(p.tile_sees)[(size_t)b * ((p.N + 31) / 32) + q0 / 32] =
+          i32x4{pub.any_lo, pub.any_hi, pub.all_lo, pub.all_hi};
+  }
+  return sb;
+}
+
+// Query row q0 + 16 qb + fr, columns 32 ks + 8 grp .. + 7, of Q~ and dO, what dP starts
+// from (-Dd), and the shift of its scores. Dd comes from the forward's fp32 output when it
+// was kept (`publish`: it is written for the dV kernel), else it is there.
+template <int D, class Form>
+__device__ __forceinline__ void load_query_rows(const ScoredParams& p, const Form& form, int b, int h, int q0,
+                                                int fr, int grp, bool publish, bf16x8_t (&qf)[QB][D / 32],
+                                                bf16x8_t (&df)[QB][D / 32], f32x4_t (&ndd)[QB],
+                                                float (&shift)[QB]) {
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int q = q0 + qb * 16 + fr, qq = min(q, p.N - 1);
+    const size_t at = (((size_t)b * p.N + qq) * p.H + h) * D + grp * 8;
+    const size_t row = ((size_t)b * p.H + h) * p.N + qq;
+    float d0 = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) {
+      qf[qb][ks] = __builtin_bit_cast(
+          bf16x8_t, *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + at + ks * 32));
+      const u32x4 gw = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.dout) + at + ks * 32);
+      df[qb][ks] = __builtin_bit_cast(bf16x8_t, gw);
+      if (p.out_f32) {
+        const f32x4_t o0 = *reinterpret_cast<const f32x4_t*>(p.out_f32 + at + ks * 32);
+        const f32x4_t o1 = *reinterpret_cast<const f32x4_t*>(p.out_f32 + at + ks * 32 + 4);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          d0 = fmaf(bf16_lo(gw[j]), o0[2 * j], fmaf(bf16_hi(gw[j]), o0[2 * j + 1], d0));
+          d0 = fmaf(bf16_lo(gw[j + 2]), o1[2 * j], fmaf(bf16_hi(gw[j + 2]), o1[2 * j + 1], d0));
+        }
+      }
+    }
+    if (p.out_f32) {
+      d0 += __shfl_xor(d0, 16);
+      d0 += __shfl_xor(d0, 32);
+      if (publish && grp == 0 && q < p.N) p.Dd[row] = d0;
+    } else {
+      d0 = p.Dd[row];
+    }
+    ndd[qb] = f32x4_t{-d0, -d0, -d0, -d0};
+    shift[qb] = form.C() - p.lse[row] * kScoredLog2e;
+  }
+}
+
+// dQ~^T += V^T dz^T for the 32 value rows from j0 on, staged at `fi` (relative rows at
+// `rows`): S^T = V Q~^T and dP^T = V dO^T share each value-row fragment read, and dz^T is
+// the last product's second operand.
+template <int D, bool CAP, bool BIAS, int ROW, class Form>
+__device__ __forceinline__ void dq_step(const Form& form, const FragOffsets<D>& fi, int rows, int j0, int q0,
+                                        int fr, int grp, bool edge, float slope, const SeenRange (&seen)[QB],
+                                        const bf16x8_t (&qf)[QB][D / 32], const bf16x8_t (&df)[QB][D / 32],
+                                        const f32x4_t (&ndd)[QB], const float (&shift)[QB],
+                                        f32x4_t (&acc)[D / 16][QB]) {
+  constexpr int KS = D / 32, DB = D / 16;
+        f32x4_t sc[2][QB], dp[2][QB];
+        bf16x8_t va[2][KS];
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int kd = 0; kd < KS; ++kd) va[hh][kd] = lds_rows(fi.s(kd) + rows + hh * 16 * ROW);
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int kd = 0; kd < KS; ++kd)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+              sc[hh][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  va[hh][kd], qf[qb][kd], kd == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[hh][qb], 0, 0, 0);
+              dp[hh][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[hh][kd], df[qb][kd],
+                                                                   kd == 0 ? ndd[qb] : dp[hh][qb], 0, 0, 0);
+            }
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, KS, 0);
+#pragma unroll
+        for (int kd = 0; kd < KS; ++kd) {
+          __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2 * QB, 0);
+          __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2 * QB * KS, 0);
+        // Lane: rows jl + 16 hh + r of query q0 + 16 qb + fr.
+        const int jl = j0 + grp * 4;
+        auto unseen = [&](int qb, int hh, int r) {
+          const int j = jl + hh * 16 + r;
+          return (j < seen[qb].lo) | (j >= seen[qb].hi);
+        };
+        bool bad = false;  // see the forward: values that a query must not see are not finite
+        if (edge) {
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                bad |= unseen(qb, hh, r) & (not_finite(sc[hh][qb][r]) | not_finite(dp[hh][qb][r]));
+          bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+          if (bad) {
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+              for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                  dp[hh][qb][r] = not_finite(sc[hh][qb][r]) ? __builtin_nanf("") : dp[hh][qb][r];
+          }
+        }
+        bf16x8_t pf[QB];
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const float dist = (float)(q0 + qb * 16 + fr - jl);
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float w, dz;
+              weigh<Form, CAP, BIAS>(form, sc[hh][qb][r], slope, dist - (float)(hh * 16 + r), dp[hh][qb][r],
+                                     shift[qb], 1.f, w, dz);
+              sc[hh][qb][r] = dz;
+            }
+        }
+        if (edge) {
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                sc[hh][qb][r] = unseen(qb, hh, r) ? 0.f : sc[hh][qb][r];
+        }
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) pf[qb] = pack8(sc[0][qb], sc[1][qb]);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          bf16x8_t a = lds_columns<ROW>(fi.t(db) + rows);
+          if (bad) a = finite_or_zero(a);
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+            acc[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf[qb], acc[db][qb], 0, 0, 0);
+        }
+}
+
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) {
+  using T = AttnTile<D, kTileRows>;
+  using Form = ScoreForm<CAP, BIAS>;
+  constexpr int KS = D / 32, DB = D / 16;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ int s_sees[4][2];
+  const HeadTile ht(p, BQ);
+  const int h = ht.h, g = ht.g, b = ht.b, qt = ht.qt;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, grp = lane >> 4;
+  const int q0 = qt * BQ + wave * 16 * QB;
+
+  SeenRange seen[QB];
+  SeenBounds sb = seen_by_rows(p, b, q0, fr, grp, h == 0, seen);
   if (q0 >= p.N) sb.any_lo = sb.any_hi = 0;
   if (lane == 0) {
-    s_sees[wave][0] = pub.any_lo;
-    s_sees[wave][1] = pub.any_hi;
-    s_sees[wave][2] = pub.all_lo;
-    s_sees[wave][3] = pub.all_hi;
+    s_sees[wave][0] = sb.any_hi > sb.any_lo ? sb.any_lo : 0x7fffffff;
+    s_sees[wave][1] = sb.any_hi;
   }
   __syncthreads();
-  if (h == 0 && threadIdx.x < 2) {
-    const int x = 2 * threadIdx.x, tile = 2 * qt + threadIdx.x, tiles = (p.N + 63) / 64;
-    if (tile < tiles) {
-      const i32x4 v{min(s_sees[x][0], s_sees[x + 1][0]), max(s_sees[x][1], s_sees[x + 1][1]),
-             max(s_sees[x][2], s_sees[x + 1][2]), min(s_sees[x][3], s_sees[x + 1][3])};
-      static_cast<i32x4*>(p.tile_sees)[(size_t)b * tiles + tile] = v;
-    }
-  }
   int lo = s_sees[0][0], hi = s_sees[0][1];
 #pragma unroll
   for (int w = 1; w < 4; ++w) {
@@ -125,47 +265,16 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) 
   for (int s = 0; s < kStages - 1; ++s)
     if (s < ntiles) issue(s, s);
 
-  // Query row q0 + 16 qb + fr, columns 32 ks + 8 grp .. + 7, of Q~ and dO. dP starts from
-  // -Dd; Dd comes from the forward's fp32 output when it was kept, else it is there.
+  const Form form(p.scale, p.cap);
+  const float slope = BIAS ? p.slopes[h] * kScoredLog2e : 0.f;
   bf16x8_t qf[QB][KS], df[QB][KS];
   f32x4_t ndd[QB], acc[DB][QB];
   float shift[QB];
-  const Form form(p.scale, p.cap);
-  const float slope = BIAS ? p.slopes[h] * kScoredLog2e : 0.f;
+  load_query_rows<D>(p, form, b, h, q0, fr, grp, true, qf, df, ndd, shift);
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const int q = q0 + qb * 16 + fr, qq = min(q, p.N - 1);
-    const size_t at = (((size_t)b * p.N + qq) * p.H + h) * D + grp * 8;
-    const size_t row = ((size_t)b * p.H + h) * p.N + qq;
-    float d0 = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      qf[qb][ks] = __builtin_bit_cast(
-          bf16x8_t, *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + at + ks * 32));
-      const u32x4 gw = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.dout) + at + ks * 32);
-      df[qb][ks] = __builtin_bit_cast(bf16x8_t, gw);
-      if (p.out_f32) {
-        const f32x4_t o0 = *reinterpret_cast<const f32x4_t*>(p.out_f32 + at + ks * 32);
-        const f32x4_t o1 = *reinterpret_cast<const f32x4_t*>(p.out_f32 + at + ks * 32 + 4);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          d0 = fmaf(bf16_lo(gw[j]), o0[2 * j], fmaf(bf16_hi(gw[j]), o0[2 * j + 1], d0));
-          d0 = fmaf(bf16_lo(gw[j + 2]), o1[2 * j], fmaf(bf16_hi(gw[j + 2]), o1[2 * j + 1], d0));
-        }
-      }
-    }
-    if (p.out_f32) {
-      d0 += __shfl_xor(d0, 16);
-      d0 += __shfl_xor(d0, 32);
-      if (grp == 0 && q < p.N) p.Dd[row] = d0;
-    } else {
-      d0 = p.Dd[row];
-    }
-    ndd[qb] = f32x4_t{-d0, -d0, -d0, -d0};
-    shift[qb] = form.C() - p.lse[row] * kScoredLog2e;
+  for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i][qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
   const FragOffsets<D> fo(fr, grp);
   KL_WAIT_VMCNT(0);
   int stage = 0;
@@ -182,91 +291,9 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) 
     const bool edge = j0 < sb.all_lo || j0 + kTileRows > sb.all_hi;
     // One 32-row step at a time, which keeps half of the tile's scores live.
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      f32x4_t sc[2][QB], dp[2][QB];
-      bf16x8_t va[2][KS];
-#pragma unroll
-      for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-        for (int kd = 0; kd < KS; ++kd) va[hh][kd] = lds_rows(fi.s(kd) + (2 * ks + hh) * 16 * T::ROW);
-#pragma unroll
-      for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-        for (int kd = 0; kd < KS; ++kd)
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb) {
-            sc[hh][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                va[hh][kd], qf[qb][kd], kd == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[hh][qb], 0, 0, 0);
-            dp[hh][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[hh][kd], df[qb][kd],
-                                                                 kd == 0 ? ndd[qb] : dp[hh][qb], 0, 0, 0);
-          }
-      __builtin_amdgcn_sched_group_barrier(kSchedDsRead, KS, 0);
-#pragma unroll
-      for (int kd = 0; kd < KS; ++kd) {
-        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2 * QB, 0);
-        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2 * QB * KS, 0);
-      // Lane: rows jl + 16 hh + r of query q0 + 16 qb + fr.
-      const int jl = j0 + 32 * ks + grp * 4;
-      auto unseen = [&](int qb, int hh, int r) {
-        const int j = jl + hh * 16 + r;
-        return (j < seen[qb].lo) | (j >= seen[qb].hi);
-      };
-      bool bad = false;  // see the forward: values that a query must not see are not finite
-      if (edge) {
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              bad |= unseen(qb, hh, r) & (not_finite(sc[hh][qb][r]) | not_finite(dp[hh][qb][r]));
-        bad = __builtin_amdgcn_ballot_w64(bad) != 0;
-        if (bad) {
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                dp[hh][qb][r] = not_finite(sc[hh][qb][r]) ? __builtin_nanf("") : dp[hh][qb][r];
-        }
-      }
-      bf16x8_t pf[QB];
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
-        const float dist = (float)(q0 + qb * 16 + fr - jl);
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float w, dz;
-            weigh<Form, CAP, BIAS>(form, sc[hh][qb][r], slope, dist - (float)(hh * 16 + r), dp[hh][qb][r],
-                                   shift[qb], 1.f, w, dz);
-            sc[hh][qb][r] = dz;
-          }
-      }
-      if (edge) {
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              sc[hh][qb][r] = unseen(qb, hh, r) ? 0.f : sc[hh][qb][r];
-      }
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) pf[qb] = pack8(sc[0][qb], sc[1][qb]);
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        bf16x8_t a = lds_columns<T::ROW>(fi.t(db) + ks * 32 * T::ROW);
-        if (bad) a = finite_or_zero(a);
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb)
-          acc[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf[qb], acc[db][qb], 0, 0, 0);
-      }
-    }
+    for (int ks = 0; ks < 2; ++ks)
+      dq_step<D, CAP, BIAS, T::ROW>(form, fi, ks * 32 * T::ROW, j0 + 32 * ks, q0, fr, grp, edge, slope, seen, qf,
+                                    df, ndd, shift, acc);
   }
   // Lane holds dQ~^T[16 db + 4 grp + r][q].
 #pragma unroll
@@ -279,6 +306,74 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) 
       const f32x4_t x = acc[db][qb] * p.scale;
       *reinterpret_cast<u32x2*>(dst + db * 16) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
     }
+  }
+}
+
+// dQ~ for few query tiles: 32 query rows of one head per workgroup, its four waves sharing
+// the 32-row value tiles through private two-stage rings; their sums are added once, in wave order.
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads, 2) void scored_dq_split_kernel(ScoredParams p) {
+  constexpr int NW = 4, RV = 32, KS = D / 32, DB = D / 16;
+  using T = AttnTile<D, RV>;
+  using Copier = WaveCopier<D, RV>;
+  using Form = ScoreForm<CAP, BIAS>;
+  constexpr int RING = 2 * T::BYTES;
+  static_assert(RING == 32 * D * 4, "a wave's results fit its ring");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const HeadTile ht(p, 32);
+  const int h = ht.h, g = ht.g, b = ht.b, q0 = ht.qt * 32;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, grp = lane >> 4;
+  SeenRange seen[QB];
+  const SeenBounds sb = seen_by_rows(p, b, q0, fr, grp, h == 0 && wave == 0, seen);
+  const bool any = sb.any_lo < sb.any_hi;
+  const int t0 = any ? sb.any_lo / RV : 0, tend = any ? (sb.any_hi + RV - 1) / RV : 0;
+  const size_t row_bytes = (size_t)p.G * D * 2;
+  const unsigned char* gV = static_cast<const unsigned char*>(p.v) + ((size_t)b * p.N * p.G + g) * D * 2;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
+  const uint32_t ring = lds0 + wave * RING;
+  const Copier cp(lane, row_bytes);
+  if (t0 + wave < tend) cp.issue(gV, row_bytes, (t0 + wave) * RV, p.N, lane, ring);
+  const Form form(p.scale, p.cap);
+  const float slope = BIAS ? p.slopes[h] * kScoredLog2e : 0.f;
+  bf16x8_t qf[QB][KS], df[QB][KS];
+  f32x4_t ndd[QB], acc[DB][QB];
+  float shift[QB];
+  load_query_rows<D>(p, form, b, h, q0, fr, grp, wave == 0, qf, df, ndd, shift);
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+    for (int i = 0; i < DB; ++i) acc[i][qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const FragOffsets<D> fo(fr, grp);
+  int stage = 0;
+  for (int t = t0 + wave; t < tend; t += NW) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the other stage has been read
+    if (t + NW < tend) {
+      cp.issue(gV, row_bytes, (t + NW) * RV, p.N, lane, ring + (stage ^ 1) * T::BYTES);
+      KL_WAIT_VMCNT(Copier::COPIES);
+    } else {
+      KL_WAIT_VMCNT(0);
+    }
+    asm volatile("" ::: "memory");
+    const FragOffsets<D> fi = fo.at(ring + stage * T::BYTES);
+    stage ^= 1;
+    const int j0 = t * RV;
+    dq_step<D, CAP, BIAS, T::ROW>(form, fi, 0, j0, q0, fr, grp, j0 < sb.all_lo || j0 + RV > sb.all_hi, slope, seen,
+                                  qf, df, ndd, shift, acc);
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) WaveSums<D>::put(ring, qb * 16 + fr, 4 * db + grp, acc[db][qb] * p.scale);
+  __syncthreads();
+  for (int e = threadIdx.x; e < 32 * D / 4; e += kThreads) {
+    const int row = e / (D / 4), piece = e % (D / 4);
+    if (q0 + row >= p.N) continue;
+    const f32x4_t x = WaveSums<D>::template get<NW>(lds0, RING, row, piece);
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.dq) + (((size_t)b * p.N + q0 + row) * p.H + h) * D +
+                              piece * 4) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
   }
 }
 
@@ -298,11 +393,17 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
   const int wg0 = kvt * BKV, kv0 = wg0 + wave * 16 * KVB;
 
   // The query tiles from the first to the last that sees one of the workgroup's rows.
-  const int tiles = (p.N + 63) / 64;
-  const i32x4* sees = static_cast<const i32x4*>(p.tile_sees) + (size_t)b * tiles;
+  const int tiles = (p.N + 63) / 64, halves = (p.N + 31) / 32;
+  const i32x4* sees = static_cast<const i32x4*>(p.tile_sees) + (size_t)b * halves;
+  // Of a 64-row tile, from its two halves; the second half of the last one may not exist.
+  auto join = [](i32x4 a, i32x4 z, bool two) {
+    i32x4 s = {min(a.x, z.x), max(a.y, z.y), max(a.z, z.z), min(a.w, z.w)};
+    if (!two) s = i32x4{a.x, a.y, a.z, 0};
+    return s;
+  };
   int first = tiles, last = 0;
   for (int t = threadIdx.x; t < tiles; t += kThreads) {
-    const i32x4 s = sees[t];
+    const i32x4 s = join(sees[2 * t], sees[min(2 * t + 1, halves - 1)], 2 * t + 1 < halves);
     if (s.x < wg0 + BKV && s.y > wg0) {
       first = min(first, t);
       last = max(last, t + 1);
@@ -343,14 +444,23 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
   // Work items: (head of the group, query tile) pairs, heads outermost; this
   // workgroup's share of them where they are split. The bounds are read as scalars
   // (an earlier kernel wrote them).
+  // A split has kLeastItems items at least: under a mask the tiles differ in what they
+  // have, and those with little are not split.
   const int per = max(last - first, 0);
-  int it = 0, items = R * per;
+  int it = 0, items = R * per, S = 1;
   if (p.S > 1) {
-    it = (int)((long)items * split / p.S);
-    items = (int)((long)items * (split + 1) / p.S);
+    S = max(1, min(p.S, items / kLeastItems));
+    if (g == 0 && split == 0 && threadIdx.x == 0) p.tile_splits[kvt * p.B + b] = S;
+    if (split >= S) return;
+    it = (int)((long)items * split / S);
+    items = (int)((long)items * (split + 1) / S);
   }
   typedef const __attribute__((address_space(4))) i32x4 const_i32x4;
-  auto bounds = [&](int i) { return ((const_i32x4*)sees)[first + i % per]; };
+  auto bounds = [&](int i) {
+    const int t = first + i % per;
+    const i32x4 a = ((const_i32x4*)sees)[2 * t], z = ((const_i32x4*)sees)[min(2 * t + 1, halves - 1)];
+    return join(a, z, 2 * t + 1 < halves);
+  };
   auto seek = [&](int i) {
     for (; i < items; ++i) {
       const i32x4 s = bounds(i);
@@ -534,7 +644,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
     const size_t at = (((size_t)b * p.N + kv) * p.G + g) * D + grp * 4;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-      if (p.S > 1)
+      if (S > 1)
         *reinterpret_cast<f32x4_t*>(p.part + (size_t)split * p.B * p.N * p.G * D + at + db * 16) = acc[db][kb];
       else
         *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.dv) + at + db * 16) =
@@ -543,13 +653,34 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
   }
 }
 
+// dv of the value tiles whose sums were split, from their fp32 partial sums in split order.
+__global__ __launch_bounds__(kThreads) void scored_sum_kernel(ScoredParams p) {
+  const int b = blockIdx.x % p.B, kvt = blockIdx.x / p.B;
+  const int S = p.tile_splits[kvt * p.B + b];
+  if (S == 1) return;
+  const long row = (long)p.G * p.D, n = (long)p.B * p.N * row;
+  const long e = ((long)blockIdx.y * kThreads + threadIdx.x) * 4;
+  if (e >= min(BKV, p.N - kvt * BKV) * row) return;
+  const long at = ((long)b * p.N + kvt * BKV) * row + e;
+  f32x4_t x = *reinterpret_cast<const f32x4_t*>(p.part + at);
+#pragma unroll 4
+  for (int s = 1; s < S; ++s) x += *reinterpret_cast<const f32x4_t*>(p.part + s * n + at);
+  *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.dv) + at) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+}
+
 template <int D, bool CAP, bool BIAS>
 hipError_t launch_form(const ScoredParams& p, hipStream_t st) {
   using T = AttnTile<D, kTileRows>;
   constexpr int dq_lds = kStages * T::BYTES;
   constexpr int dv_lds = 4 * T::BYTES + 2048;  // two stages of Q~ and dO tiles and their rows
-  hipLaunchKernelGGL((scored_dq_kernel<D, CAP, BIAS>), dim3((unsigned)p.H * p.B * ((p.N + BQ - 1) / BQ)),
-                     dim3(kThreads), dq_lds, st, p);
+  if (scored_few_query_tiles(p)) {
+    constexpr int split_lds = 4 * 2 * AttnTile<D, 32>::BYTES;
+    hipLaunchKernelGGL((scored_dq_split_kernel<D, CAP, BIAS>), dim3((unsigned)p.H * p.B * ((p.N + 31) / 32)),
+                       dim3(kThreads), split_lds, st, p);
+  } else {
+    hipLaunchKernelGGL((scored_dq_kernel<D, CAP, BIAS>), dim3((unsigned)p.H * p.B * ((p.N + BQ - 1) / BQ)),
+                       dim3(kThreads), dq_lds, st, p);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (dv_lds > 65536) {
@@ -561,7 +692,9 @@ hipError_t launch_form(const ScoredParams& p, hipStream_t st) {
                      dim3((unsigned)p.G * p.B * p.S * ((p.N + BKV - 1) / BKV)), dim3(kThreads), dv_lds, st, p);
   e = hipGetLastError();
   if (e != hipSuccess || p.S == 1) return e;
-  return launch_sum_partials_bf16(p.part, p.S, (size_t)p.B * p.N * p.G * D, p.dv, st);
+  const dim3 grid(p.B * ((p.N + BKV - 1) / BKV), (unsigned)(((long)BKV * p.G * D / 4 + kThreads - 1) / kThreads));
+  hipLaunchKernelGGL(scored_sum_kernel, grid, dim3(kThreads), 0, st, p);
+  return hipGetLastError();
 }
 
 template <int D>

@@ -282,4 +282,55 @@ __device__ __forceinline__ bool soften(const Form& form, f32x4_t (&sc)[NB][QB], 
   return bad;
 }
 
+// Merge of the NW waves of a workgroup, each with partial results of the same 16 QB rows:
+// the sums are scaled to the rows' common reference and added in wave order. A wave that
+// saw nothing of a row has reference -inf (and sums of zero). Every wave's place of LDS
+// at ring0 + wave * stride holds its results.
+template <int D, int QB, int NW>
+struct WaveMerge {
+  float (*ml)[16 * QB][2];
+  uint32_t ring0, stride;
+  int wave, fr, grp;
+  __device__ __forceinline__ WaveMerge(float (*s_ml)[16 * QB][2], uint32_t ring0_, uint32_t stride_, int wave_,
+                                       int fr_, int grp_)
+      : ml(s_ml), ring0(ring0_), stride(stride_), wave(wave_), fr(fr_), grp(grp_) {}
+  __device__ __forceinline__ float top(int row) const {
+    float x = ml[0][row][0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) x = fmaxf(x, ml[w][row][0]);
+    return x;
+  }
+  // l: this lane's part of the weight sums.
+  __device__ __forceinline__ void put(const float (&m)[QB], const float (&l)[QB], const f32x4_t (&o)[D / 16][QB]) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wave's tiles have been read
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      float sum = l[qb] + __shfl_xor(l[qb], 16);
+      sum += __shfl_xor(sum, 32);
+      if (grp == 0) {
+        ml[wave][qb * 16 + fr][0] = m[qb];
+        ml[wave][qb * 16 + fr][1] = sum;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const float mm = top(qb * 16 + fr), f = fast_exp2(m[qb] - (mm == -INFINITY ? 0.f : mm));
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db)
+        WaveSums<D>::put(ring0 + wave * stride, qb * 16 + fr, 4 * db + grp, o[db][qb] * f);
+    }
+    __syncthreads();
+  }
+  // Four columns of a row, its reference and its weight sum.
+  __device__ __forceinline__ f32x4_t get(int row, int piece, float& mm, float& sum) const {
+    mm = top(row);
+    const float ms = mm == -INFINITY ? 0.f : mm;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) sum += ml[w][row][1] * fast_exp2(ml[w][row][0] - ms);
+    return WaveSums<D>::template get<NW>(ring0, stride, row, piece);
+  }
+};
+
 }  // namespace kl

@@ -209,6 +209,141 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p)
   }
 }
 
+// The same for few query tiles (short prompts, few heads): a workgroup owns 32 query rows
+// of one head and its four waves share the 32-row value tiles, tile t to wave t % 4, each
+// through a private two-stage ring with no barrier, and meet once to merge.
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads, 2) void scored_fwd_split_kernel(ScoredParams p) {
+  constexpr int QB = 2, NW = 4, RV = 32, BQ = 16 * QB, KS = D / 32, DB = D / 16;
+  using T = AttnTile<D, RV>;
+  using Copier = WaveCopier<D, RV>;
+  using Form = ScoreForm<CAP, BIAS>;
+  constexpr int RING = 2 * T::BYTES;
+  static_assert(RING == BQ * D * 4, "a wave's results fit its ring");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ float s_ml[NW][BQ][2];
+  const HeadTile ht(p, BQ);
+  const int h = ht.h, g = ht.g, b = ht.b, q0 = ht.qt * BQ;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, grp = lane >> 4;
+  SeenRange seen[QB];
+  SeenBounds sb;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    seen[qb] = seen_range(p, b, min(q0 + qb * 16 + fr, p.N - 1));
+    sb.add(seen[qb]);
+  }
+  sb.over_lanes(15);
+  sb.make_uniform();
+  const bool any = sb.any_lo < sb.any_hi;
+  const int t0 = any ? sb.any_lo / RV : 0, tend = any ? (sb.any_hi + RV - 1) / RV : 0;
+
+  const size_t row_bytes = (size_t)p.G * D * 2;
+  const unsigned char* gV = static_cast<const unsigned char*>(p.v) + ((size_t)b * p.N * p.G + g) * D * 2;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
+  const uint32_t ring = lds0 + wave * RING;
+  const Copier cp(lane, row_bytes);
+  if (t0 + wave < tend) cp.issue(gV, row_bytes, (t0 + wave) * RV, p.N, lane, ring);
+  bf16x8_t qf[QB][KS];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const uint16_t* src = static_cast<const uint16_t*>(p.q) +
+                          (((size_t)b * p.N + min(q0 + qb * 16 + fr, p.N - 1)) * p.H + h) * D + grp * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      qf[qb][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(src + ks * 32));
+  }
+  const Form form(p.scale, p.cap);
+  const float slope = BIAS ? p.slopes[h] * kScoredLog2e : 0.f;
+  f32x4_t o[DB][QB];
+  float m[QB], l[QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    m[qb] = -INFINITY;
+    l[qb] = 0.f;
+#pragma unroll
+    for (int i = 0; i < DB; ++i) o[i][qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const FragOffsets<D> fo(fr, grp);
+  int stage = 0;
+  for (int t = t0 + wave; t < tend; t += NW) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the other stage has been read
+    if (t + NW < tend) {
+      cp.issue(gV, row_bytes, (t + NW) * RV, p.N, lane, ring + (stage ^ 1) * T::BYTES);
+      KL_WAIT_VMCNT(Copier::COPIES);
+    } else {
+      KL_WAIT_VMCNT(0);
+    }
+    asm volatile("" ::: "memory");
+    const int j0 = t * RV;
+    const FragOffsets<D> fi = fo.at(ring + stage * T::BYTES);
+    stage ^= 1;
+    if (j0 >= sb.any_hi || j0 + RV <= sb.any_lo) continue;
+    f32x4_t sc[2][QB];
+    bf16x8_t sa[2][KS];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) sa[kb][ks] = lds_rows(fi.s(ks) + kb * 16 * T::ROW);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+          sc[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              sa[kb][ks], qf[qb][ks], ks == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[kb][qb], 0, 0, 0);
+    const int jl = j0 + grp * 4;
+    const bool bad = soften<D, 2, QB>(
+        form, sc, o, m, l, j0 < sb.all_lo || j0 + RV > sb.all_hi,
+        [&](int qb, int kb, int r) {
+          const int j = jl + kb * 16 + r;
+          return (j < seen[qb].lo) | (j >= seen[qb].hi);
+        },
+        [&](float x, int qb, int kb, int r) {
+          return fmaf(-slope, fabsf((float)(q0 + qb * 16 + fr - jl) - (float)(kb * 16 + r)), x);
+        });
+    bf16x8_t pf[QB], av[DB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) pf[qb] = pack8(sc[0][qb], sc[1][qb]);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) av[db] = lds_columns<T::ROW>(fi.t(db));
+    if (bad) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) av[db] = finite_or_zero(av[db]);
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+        o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[db], pf[qb], o[db][qb], 0, 0, 0);
+  }
+  WaveMerge<D, QB, NW> merge(s_ml, lds0, RING, wave, fr, grp);
+  merge.put(m, l, o);
+  for (int e = threadIdx.x; e < BQ * D / 4; e += kThreads) {
+    const int row = e / (D / 4), piece = e % (D / 4);
+    if (q0 + row >= p.N) continue;
+    float mm, sum;
+    f32x4_t x = merge.get(row, piece, mm, sum);
+    const bool none = sum == 0.f;
+    x *= none ? 0.f : 1.f / sum;
+    const size_t at = (((size_t)b * p.N + q0 + row) * p.H + h) * D + piece * 4;
+    const size_t lrow = ((size_t)b * p.H + h) * p.N + q0 + row;
+    if (p.Dd) {  // for the backward, as in the kernel above; a row's pieces lie in D / 4 lanes
+      const u32x2 w = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p.dout) + at);
+      float d0 = fmaf(bf16_lo(w[0]), x[0], bf16_hi(w[0]) * x[1]);
+      d0 = fmaf(bf16_lo(w[1]), x[2], fmaf(bf16_hi(w[1]), x[3], d0));
+      d0 = group_sum<D / 4>(d0);
+      if (piece == 0) p.Dd[lrow] = d0;
+      continue;
+    }
+    if (p.lse && piece == 0) p.lse[lrow] = none ? -INFINITY : (mm + __log2f(sum)) * kScoredLn2;
+    if (p.out_f32) *reinterpret_cast<f32x4_t*>(p.out_f32 + at) = x;
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+  }
+}
+
 template <int D, int QB, bool CAP, bool BIAS>
 hipError_t launch_qb(const ScoredParams& p, hipStream_t st) {
   constexpr int BQ = 64 * QB, lds = kStages * AttnTile<D, kTileRows>::BYTES;
@@ -217,13 +352,29 @@ hipError_t launch_qb(const ScoredParams& p, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <int D, bool CAP, bool BIAS>
+hipError_t launch_form(const ScoredParams& p, hipStream_t st) {
+  if (scored_few_query_tiles(p)) {
+    constexpr int lds = 4 * 2 * AttnTile<D, 32>::BYTES;
+    hipLaunchKernelGGL((scored_fwd_split_kernel<D, CAP, BIAS>), dim3((unsigned)p.H * p.B * ((p.N + 31) / 32)),
+                       dim3(kThreads), lds, st, p);
+    return hipGetLastError();
+  }
+  return launch_qb<D, 2, CAP, BIAS>(p, st);
+}
+
 template <int D>
 hipError_t launch_d(const ScoredParams& p, hipStream_t st) {
-  if (p.cap > 0.f) return p.slopes ? launch_qb<D, 2, true, true>(p, st) : launch_qb<D, 2, true, false>(p, st);
-  return p.slopes ? launch_qb<D, 2, false, true>(p, st) : launch_qb<D, 2, false, false>(p, st);
+  if (p.cap > 0.f) return p.slopes ? launch_form<D, true, true>(p, st) : launch_form<D, true, false>(p, st);
+  return p.slopes ? launch_form<D, false, true>(p, st) : launch_form<D, false, false>(p, st);
 }
 
 }  // namespace
+
+bool scored_few_query_tiles(const ScoredParams& p) {
+  const long heads = (long)p.H * p.B;
+  return heads * ((p.N + 127) / 128) < 512;
+}
 
 hipError_t launch_scored_forward_bf16(const ScoredParams& p, hipStream_t st) {
   return p.D == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);

@@ -231,41 +231,13 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(TreeParams p) {
         o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[db], pf[qb], o[db][qb], 0, 0, 0);
   }
 
-  // Merge in wave order: each wave's reference and weight sum, then its sums scaled to
-  // the common reference. A wave that saw nothing of a row has reference -inf.
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    l[qb] += __shfl_xor(l[qb], 16);
-    l[qb] += __shfl_xor(l[qb], 32);
-    if (grp == 0) {
-      s_ml[wave][qb * 16 + fr][0] = m[qb];
-      s_ml[wave][qb * 16 + fr][1] = l[qb];
-    }
-  }
-  __syncthreads();
-  auto top = [&](int row) {
-    float x = s_ml[0][row][0];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) x = fmaxf(x, s_ml[w][row][0]);
-    return x;
-  };
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const float mm = top(qb * 16 + fr), ms = mm == -INFINITY ? 0.f : mm;
-    const float f = fast_exp2(m[qb] - ms);
-#pragma unroll
-    for (int db = 0; db < DB; ++db) WaveSums<D>::put(ring, qb * 16 + fr, 4 * db + grp, o[db][qb] * f);
-  }
-  __syncthreads();
+  WaveMerge<D, QB, NW> merge(s_ml, lds0, RING, wave, fr, grp);
+  merge.put(m, l, o);
   for (int e = threadIdx.x; e < BQ * D / 4; e += kThreads) {
     const int row = e / (D / 4), piece = e % (D / 4), mr = m0 + row;
     if (mr >= M) continue;
-    const float mm = top(row), ms = mm == -INFINITY ? 0.f : mm;
-    float sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) sum += s_ml[w][row][1] * fast_exp2(s_ml[w][row][0] - ms);
-    const f32x4_t x = WaveSums<D>::template get<NW>(lds0, RING, row, piece);
+    float mm, sum;
+    const f32x4_t x = merge.get(row, piece, mm, sum);
     if (sp.S == 1) {
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       uint16_t* dst = static_cast<uint16_t*>(p.out) +
