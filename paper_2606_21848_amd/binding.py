@@ -184,10 +184,7 @@ class ValueCache:
             d.block_table = block_table.data_ptr()
         _ptr(data)
         self.desc = d
-
-    @property
-    def ref(self):
-        return ctypes.byref(self.desc)
+        self.ref = ctypes.byref(d)
 
 
 def decode_workspace_bytes(cache: ValueCache, B: int, H: int, chunk_rows: int = 0) -> int:
@@ -559,13 +556,15 @@ def _like(t, shape, dtype, dev, what):
     """t as an argument: None, or a tensor of this shape and type on that device."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape):
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    if t.shape != shape:
         raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
     if t.get_device() != dev:
         raise ValueError(f"{what} is on another device than the first argument")
-    return _ptr(t)
+    raise ValueError(f"{what} must be contiguous")
 
 
 def _call(dev: int, fn, *args):
@@ -589,29 +588,34 @@ class Scoring:
                  causal: bool = True):
         self.cap, self.slopes, self.first, self.last, self.causal = cap, slopes, first, last, causal
         self.desc = KLScoring(cap, _ptr(slopes), _ptr(first), _ptr(last), int(causal))
+        self._ref = ctypes.byref(self.desc)
 
     def checked(self, B: int, N: int, H: int, dev: int):
         """The descriptor, once its tensors fit a call on [B, N, H, d] tensors."""
-        _like(self.slopes, (H,), torch.float32, dev, "slopes")
-        _like(self.first, (B, N), torch.int32, dev, "first")
-        _like(self.last, (B, N), torch.int32, dev, "last")
-        return ctypes.byref(self.desc)
+        if self.slopes is not None:
+            _like(self.slopes, (H,), torch.float32, dev, "slopes")
+        if self.first is not None:
+            _like(self.first, (B, N), torch.int32, dev, "first")
+        if self.last is not None:
+            _like(self.last, (B, N), torch.int32, dev, "last")
+        return self._ref
 
 
 def keyless_scored_forward(q_routed: torch.Tensor, v: torch.Tensor, scoring: Scoring,
                            scale: float = 0.0, out=None, lse=None, out_f32=None):
     """keyless_attention_forward with the scores and masks of ``scoring``; returns (out, lse)."""
     load()
-    B, N, H, dk = q_routed.shape
+    like_q = q_routed.shape
+    B, N, H, dk = like_q
     G, dev, dt = v.shape[2], q_routed.get_device(), q_routed.dtype
     if out is None:
         out = torch.empty_like(q_routed)
     if lse is None:
-        lse = torch.empty((B, H, N), dtype=torch.float32, device=q_routed.device)
+        lse = q_routed.new_empty((B, H, N), dtype=torch.float32)
     _call(dev, _lib.keyless_scored_forward, _ptr(q_routed), _like(v, (B, N, G, dk), dt, dev, "v"),
           scoring.checked(B, N, H, dev), B, N, H, G, dk, scale, _dt(q_routed),
-          _like(out, (B, N, H, dk), dt, dev, "out"), _like(lse, (B, H, N), torch.float32, dev, "lse"),
-          _like(out_f32, (B, N, H, dk), torch.float32, dev, "out_f32"))
+          _like(out, like_q, dt, dev, "out"), _like(lse, (B, H, N), torch.float32, dev, "lse"),
+          _like(out_f32, like_q, torch.float32, dev, "out_f32"))
     return out, lse
 
 
@@ -653,7 +657,7 @@ def tree_decode_workspace_bytes(cache: ValueCache, B: int, T: int, H: int) -> in
 
 
 def _per_sequence(cache: ValueCache, t: torch.Tensor, B: int, dev: int, what: str):
-    rows = cache.block_table if cache.block_table is not None else cache.data
+    rows = cache.data if cache.block_table is None else cache.block_table
     if rows.shape[0] != B:
         raise ValueError(f"the cache holds {rows.shape[0]} sequences, not {B}")
     return _like(t, (B,), torch.int32, dev, what)
@@ -667,9 +671,10 @@ def keyless_tree_decode(q_routed: torch.Tensor, cache: ValueCache, lengths_befor
     the drafted rows that ``tree`` lets each see (int64 [B, T], bit u of word t: token t sees
     drafted row u, at position lengths_before[b] + u of the cache; None: a chain)."""
     load()
-    B, T, H, dk = q_routed.shape
-    dev = q_routed.get_device()
-    if dk != cache.desc.d_head or q_routed.dtype != cache.data.dtype:
+    like_q = q_routed.shape
+    B, T, H, dk = like_q
+    dev, dt = q_routed.get_device(), cache.data.dtype
+    if dk != cache.data.shape[3] or q_routed.dtype is not dt:
         raise ValueError("q_routed and the cache differ in d_head or dtype")
     if out is None:
         out = torch.empty_like(q_routed)
@@ -680,7 +685,7 @@ def keyless_tree_decode(q_routed: torch.Tensor, cache: ValueCache, lengths_befor
           _per_sequence(cache, lengths_before, B, dev, "lengths_before"),
           _like(tree, (B, T), torch.int64, dev, "tree"), B, T, H, cap,
           _like(slopes, (H,), torch.float32, dev, "slopes"), scale,
-          _like(out, q_routed.shape, q_routed.dtype, dev, "out"), _ptr(workspace),
+          _like(out, like_q, dt, dev, "out"), _ptr(workspace),
           workspace.numel() * workspace.element_size())
     return out
 

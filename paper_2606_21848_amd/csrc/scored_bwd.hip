@@ -27,7 +27,7 @@ constexpr int kThreads = 256;
 constexpr int kTileRows = 64;
 constexpr int kStages = 3;           // value tiles in LDS (dQ~)
 constexpr int QB = 2, BQ = 64 * QB;  // 16-row query blocks per wave, query rows per workgroup (dQ~)
-constexpr int kLeastItems = 4;       // (head, query tile) pairs of a split of the dV sums
+constexpr int kLeastItems = 2;       // (head, query tile) pairs of a split of the dV sums
 constexpr int KVB = 3, BKV = 64 * KVB;  // value blocks per wave, value rows per workgroup (dV)
 
 // One 4-byte-per-lane copy from global memory straight into LDS.
