@@ -1388,20 +1388,35 @@ int keyless_scored_backward(const void* q_routed, const void* v, const void* out
 namespace {
 
 // Work split of a drafted-token decode, from the shapes alone (the kernels share the
-// rows out from the lengths): about two workgroups per CU, chunks of at least 128 rows;
-// a capacity of at most 1024 rows is one chunk, without partial results or a merge.
+// rows out from the lengths): the workgroups that the chip runs at once, two per CU (one
+// of 64 query rows).
+//  - A capacity of at most 1024 rows is one piece per sequence, without a merge.
+//  - At most kSmallBatch sequences: fixed pieces of at least 128 rows.
+//  - Otherwise even pieces of all rows.
 struct TreePlan {
-  int chunks, least;
+  int chunks, least, per, block_rows;
   size_t ml, total;
 };
 TreePlan plan_tree(const kl_value_cache* c, int B, int T, int H) {
-  TreePlan pl{1, 1 << 30, 0, 0};
-  if (cache_capacity(c) <= 1024) return pl;
-  const long M = (long)T * (H / c->G), rows_per = c->dtype == KL_BF16 ? 32 : 16;
-  const long blocks = (M + rows_per - 1) / rows_per;
-  pl.chunks = (int)std::max(1L, kBalancedWorkgroups / (c->G * blocks));
+  TreePlan pl{};
+  const long M = (long)T * (H / c->G), tiles = (cache_capacity(c) + 31) / 32;
+  pl.block_rows = c->dtype != KL_BF16 || M <= 16 ? 16 : M <= 32 ? 32 : 64;
+  const long blocks = (M + pl.block_rows - 1) / pl.block_rows * c->G;
+  const long slots = (pl.block_rows == 64 ? kComputeUnits : 2 * kComputeUnits);
+  pl.chunks = 1;
   pl.least = 4;
-  const size_t rows = (size_t)(pl.chunks + B) * c->G * M;
+  if (tiles <= 32) {
+    pl.per = 32;
+    return pl;
+  }
+  if (B <= kSmallBatch) {
+    pl.per = (int)std::max(4L, (tiles * B * blocks + slots - 1) / slots);
+    pl.chunks = (int)((tiles + pl.per - 1) / pl.per);
+    if (pl.chunks == 1) return pl;
+  } else {
+    pl.chunks = (int)std::max(1L, slots / blocks);
+  }
+  const size_t rows = (size_t)(pl.per > 0 ? (long)pl.chunks * B : pl.chunks + (long)B) * c->G * M;
   pl.ml = align256(rows * c->d_head * sizeof(float));
   pl.total = pl.ml + align256(rows * 2 * sizeof(float));
   return pl;
@@ -1439,8 +1454,9 @@ int keyless_tree_decode(const void* q_routed, const kl_value_cache* cache,
     return fail(KL_ERR_INVALID_ARG, "%s: scale must be finite and >= 0 (0 = 1/sqrt(d_head))", who);
   if (cache_capacity(cache) > (1 << 30))
     return fail(KL_ERR_UNSUPPORTED, "%s: capacity per sequence too large", who);
-  if ((double)B * H * T >= 2147483648.0)
-    return fail(KL_ERR_UNSUPPORTED, "%s: B * H * T too large", who);
+  // The grid has one workgroup per 16 query rows of a group and piece, 1024 pieces at most.
+  if ((double)B * H * T >= 2147483648.0 / 1024 || (double)B * cache_capacity(cache) >= 2147483648.0 * 16)
+    return fail(KL_ERR_UNSUPPORTED, "%s: B * H * T or B * capacity too large", who);
   if (B == 0) return KL_OK;
   const size_t need = keyless_tree_decode_workspace_size(cache, B, T, H);
   if (need && (!ws || ws_bytes < need))
@@ -1471,6 +1487,8 @@ int keyless_tree_decode(const void* q_routed, const kl_value_cache* cache,
   const TreePlan pl = plan_tree(cache, B, T, H);
   p.chunks = pl.chunks;
   p.least = pl.least;
+  p.per = pl.per;
+  p.block_rows = pl.block_rows;
   if (need) {
     p.part = static_cast<float*>(ws);
     p.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.ml);

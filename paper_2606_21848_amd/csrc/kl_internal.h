@@ -311,11 +311,13 @@ struct TreeParams {
   bool paged;
   int L_max, block_shift, num_blocks, max_blocks;
   float scale, cap;
-  // Work split: at most chunks + B chunks of at least `least` 32-row tiles each, and
-  // the partial results of those of split sequences (null: every sequence is one chunk).
-  int chunks, least;
-  float* part;     // [chunks + B, G, T H / G, D]
-  float* part_ml;  // [chunks + B, G, T H / G, 2]
+  // Work split over pieces of 32-row tiles (tree_device.h): `chunks` pieces of all tiles of
+  // at least `least` tiles each (per 0), or of each sequence, of `per` tiles each; and the
+  // partial results of sequences in several pieces, by slot (null: there are none).
+  int chunks, least, per;
+  int block_rows;  // query rows per workgroup (bf16: 16, 32 or 64; fp32: 16)
+  float* part;     // [slots, G, T H / G, D]
+  float* part_ml;  // [slots, G, T H / G, 2]
 };
 hipError_t launch_tree_decode_bf16(const TreeParams& p, hipStream_t stream);
 hipError_t launch_tree_decode_f32(const TreeParams& p, hipStream_t stream);

@@ -383,90 +383,93 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeParams p) {
   const int R = p.H / p.G, M = p.T * R, blocks = (M + 15) / 16;
   const int kg = blockIdx.x % p.G, m0 = (int)(blockIdx.x / p.G % blocks) * 16;
   const int c = blockIdx.x / p.G / blocks;
-  TreeSpan sp;
-  if (!tree_span(p, lane, c, -1, sp)) return;
   float* const tile = lds_f32 + wave * Block<D>::FLOATS;
-  const int row0 = sp.tile0 * kTreeTile;
-  const int nblk = (min(sp.rows - row0, sp.tiles * kTreeTile) + 15) / 16;
-  const float* data = static_cast<const float*>(p.data);
-  // The rows of block t, of which `n` exist; none outside the cache.
-  auto rows_of = [&](int t, int& n) {
-    const int j = row0 + t * 16;
-    n = min(sp.rows - j, 16);
-    if constexpr (PAGED) {
-      const int blk =
-          ((const __attribute__((address_space(4))) int*)p.table)[(size_t)sp.b * p.max_blocks + (j >> p.block_shift)];
-      const bool ok = blk >= 0 && blk < p.num_blocks;
-      if (!ok) n = 0;
-      return data + ((((size_t)(ok ? blk : 0) * p.G + kg) << p.block_shift) + (j & ((1 << p.block_shift) - 1))) * D;
-    } else {
-      return data + (((size_t)sp.b * p.G + kg) * p.L_max + j) * D;
-    }
-  };
-  f32x4_t v[S], q[S], o[S][1];
-  int live = 0, live_next = 0;
-  if (wave < nblk) {
-    const float* V = rows_of(wave, live_next);
-    load_rows<D>(V, D, r, live_next, g, v);
-  }
-  const int mr = min(m0 + r, M - 1), tok = mr / R;
-  load_rows<D>(static_cast<const float*>(p.q) + (((size_t)sp.b * p.T + tok) * p.H + kg * R + mr % R) * D, D, 0, 1,
-               g, q);
-  const uint64_t word = tree_word(p, sp.b, tok);
-  const int place = tree_depth(word, tok);
-  float slope = 0.f;
-  if constexpr (BIAS) {
-    slope = p.slopes[kg * R + mr % R] * kScoredLog2e;
-    for (int t = threadIdx.x; t < p.T; t += NW * 64) s_depth[t] = tree_depth(tree_word(p, sp.b, t), t);
-    __syncthreads();
-  }
   const ExactForm<CAP, BIAS> form(p.scale, p.cap);
-  float m[1] = {-INFINITY}, l[1] = {0.f};
-#pragma unroll
-  for (int s = 0; s < S; ++s) o[s][0] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int t = wave; t < nblk; t += NW) {
-    const int j0 = row0 + t * 16;
-    live = live_next;
-    stage_rows<D>(tile, r, g, v);
-    const f32x4_t sc = dot_rows<D>(v, q, f32x4_t{0.f, 0.f, 0.f, 0.f});
-    if (t + NW < nblk) {
-      const float* V = rows_of(t + NW, live_next);
+  TreeWalk walk(p, lane, c);
+  TreeSeg sp;
+  while (walk.next(p, lane, sp)) {
+    const int row0 = sp.tile0 * kTreeTile;
+    const int nblk = (min(sp.rows - row0, sp.tiles * kTreeTile) + 15) / 16;
+    const float* data = static_cast<const float*>(p.data);
+    // The rows of block t, of which `n` exist; none outside the cache.
+    auto rows_of = [&](int t, int& n) {
+      const int j = row0 + t * 16;
+      n = min(sp.rows - j, 16);
+      if constexpr (PAGED) {
+        const int blk =
+            ((const __attribute__((address_space(4))) int*)p.table)[(size_t)sp.b * p.max_blocks + (j >> p.block_shift)];
+        const bool ok = blk >= 0 && blk < p.num_blocks;
+        if (!ok) n = 0;
+        return data + ((((size_t)(ok ? blk : 0) * p.G + kg) << p.block_shift) + (j & ((1 << p.block_shift) - 1))) * D;
+      } else {
+        return data + (((size_t)sp.b * p.G + kg) * p.L_max + j) * D;
+      }
+    };
+    f32x4_t v[S], q[S], o[S][1];
+    int live = 0, live_next = 0;
+    if (wave < nblk) {
+      const float* V = rows_of(wave, live_next);
       load_rows<D>(V, D, r, live_next, g, v);
     }
-    const bool edge = j0 + 16 > sp.n || live < 16;
-    const int jl = j0 + 4 * g;
-    take_block<D>(
-        form, tile, r, g, sc, o, m, l, edge,
-        [&](int, int, int i) {
-          const int u = jl + i - sp.n;
-          return (4 * g + i >= live) | ((u >= 0) & ((word >> (u & 63) & 1) == 0));
-        },
-        [&](float x, int, int, int i) {
-          const int j = jl + i;
-          int d = sp.n + place - j;
-          if (BIAS && edge && j >= sp.n) d = abs(place - s_depth[min(j - sp.n, p.T - 1)]);
-          return fmaf(-slope, (float)d, x);
-        });
-  }
-  f32x4_t acc[S];
-#pragma unroll
-  for (int s = 0; s < S; ++s) acc[s] = o[s][0];
-  merge_waves_f32<D>(lds_f32, tile, s_ml, wave, r, g, m[0], l[0], acc,
-                     [&](int row, int col, f32x4_t x, float mx, float sum) {
-    const int m1 = m0 + row;
-    if (m1 >= M) return;
-    if (sp.S == 1) {
-      float* dst = static_cast<float*>(p.out) + (((size_t)sp.b * p.T + m1 / R) * p.H + kg * R + m1 % R) * D + col;
-      *reinterpret_cast<f32x4_t*>(dst) = x * (sum == 0.f ? 0.f : 1.f / sum);
-    } else {
-      *reinterpret_cast<f32x4_t*>(tree_part(p, c, kg, m1) + col) = x;
-      if (col == 0) {
-        float* ml = tree_part_ml(p, c, kg, m1);
-        ml[0] = mx;
-        ml[1] = sum;
-      }
+    const int mr = min(m0 + r, M - 1), tok = mr / R;
+    load_rows<D>(static_cast<const float*>(p.q) + (((size_t)sp.b * p.T + tok) * p.H + kg * R + mr % R) * D, D, 0, 1,
+                 g, q);
+    const uint64_t word = tree_word(p, sp.b, tok);
+    const int place = tree_depth(word, tok);
+    float slope = 0.f;
+    if constexpr (BIAS) {
+      slope = p.slopes[kg * R + mr % R] * kScoredLog2e;
+      for (int t = threadIdx.x; t < p.T; t += NW * 64) s_depth[t] = tree_depth(tree_word(p, sp.b, t), t);
+      __syncthreads();
     }
-  });
+    float m[1] = {-INFINITY}, l[1] = {0.f};
+#pragma unroll
+    for (int s = 0; s < S; ++s) o[s][0] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int t = wave; t < nblk; t += NW) {
+      const int j0 = row0 + t * 16;
+      live = live_next;
+      stage_rows<D>(tile, r, g, v);
+      const f32x4_t sc = dot_rows<D>(v, q, f32x4_t{0.f, 0.f, 0.f, 0.f});
+      if (t + NW < nblk) {
+        const float* V = rows_of(t + NW, live_next);
+        load_rows<D>(V, D, r, live_next, g, v);
+      }
+      const bool edge = j0 + 16 > sp.n || live < 16;
+      const int jl = j0 + 4 * g;
+      take_block<D>(
+          form, tile, r, g, sc, o, m, l, edge,
+          [&](int, int, int i) {
+            const int u = jl + i - sp.n;
+            return (4 * g + i >= live) | ((u >= 0) & ((word >> (u & 63) & 1) == 0));
+          },
+          [&](float x, int, int, int i) {
+            const int j = jl + i;
+            int d = sp.n + place - j;
+            if (BIAS && edge && j >= sp.n) d = abs(place - s_depth[min(j - sp.n, p.T - 1)]);
+            return fmaf(-slope, (float)d, x);
+          });
+    }
+    f32x4_t acc[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) acc[s] = o[s][0];
+    merge_waves_f32<D>(lds_f32, tile, s_ml, wave, r, g, m[0], l[0], acc,
+                       [&](int row, int col, f32x4_t x, float mx, float sum) {
+      const int m1 = m0 + row;
+      if (m1 >= M) return;
+      if (sp.whole) {
+        float* dst = static_cast<float*>(p.out) + (((size_t)sp.b * p.T + m1 / R) * p.H + kg * R + m1 % R) * D + col;
+        *reinterpret_cast<f32x4_t*>(dst) = x * (sum == 0.f ? 0.f : 1.f / sum);
+      } else {
+        *reinterpret_cast<f32x4_t*>(tree_part(p, sp.slot, kg, m1) + col) = x;
+        if (col == 0) {
+          float* ml = tree_part_ml(p, sp.slot, kg, m1);
+          ml[0] = mx;
+          ml[1] = sum;
+        }
+      }
+    });
+    __syncthreads();  // the results have been read: the next segment may fill their place
+  }
 }
 
 template <class K, class P>
@@ -513,7 +516,7 @@ hipError_t tree(const TreeParams& p, hipStream_t st) {
   const hipError_t e = pick_form(p, [&](auto cap, auto bias) {
     static std::atomic<uint32_t> done_p{0}, done_c{0};
     constexpr bool C = decltype(cap)::value, A = decltype(bias)::value;
-    const unsigned grid = (unsigned)(p.chunks + p.B) * ((p.T * (p.H / p.G) + 15) / 16) * p.G;
+    const unsigned grid = (unsigned)p.chunks * (p.per > 0 ? p.B : 1) * ((p.T * (p.H / p.G) + 15) / 16) * p.G;
     const int lds = NW * Block<D>::FLOATS * 4;
     return p.paged ? launch(tree_kernel<D, C, A, true>, p, grid, lds, done_p, st)
                    : launch(tree_kernel<D, C, A, false>, p, grid, lds, done_c, st);

@@ -4,12 +4,10 @@
 // the tree says. Scores with a tanh cap and a distance bias as in the scored attention.
 //
 // The T queries of all H / G heads of a group read the same rows, so a workgroup takes a
-// block of 16 QB of these T H / G query rows over one chunk of a sequence's rows: the
-// matrix cores work on whole 16-row blocks and a cached row crosses HBM once for all
-// tokens and heads of a block (blocks of one chunk run side by side on one XCD where G is
-// a multiple of 8, and meet its rows in L2). The four waves share the chunk's 32-row tiles, tile
-// t to wave t % 4, each through a private two-stage LDS ring with no barrier, and meet
-// once to merge. Only tiles that reach into the draft or past its end are masked.
+// block of these T H / G query rows over a piece of the cache: the matrix cores work on
+// whole 16-row blocks and a cached row crosses HBM once for all tokens and heads of a
+// block (blocks of one piece run side by side on one XCD where G is a multiple of 8, and
+// meet its rows in L2). Only tiles that reach into the draft or past its end are masked.
 
 #include "attn_tile.h"
 #include "scored_device.h"
@@ -32,7 +30,7 @@ struct CacheTiles {
   const __attribute__((address_space(4))) int* table;
   int rows, shift, num_blocks;
   size_t block_bytes;
-  __device__ __forceinline__ CacheTiles(const TreeParams& p, const TreeSpan& sp, int g, int lane)
+  __device__ __forceinline__ CacheTiles(const TreeParams& p, const TreeSeg& sp, int g, int lane)
       : lane_row(lane / T::CHUNKS), rows(sp.rows), shift(p.block_shift), num_blocks(p.num_blocks) {
 #pragma unroll
     for (int c = 0; c < COPIES; ++c)
@@ -53,31 +51,29 @@ struct CacheTiles {
     const int blk = table[j >> shift];
     return blk < num_blocks ? blk : -1;
   }
-  // Copies the tile from row j0 on, whose halves lie in blocks b0 and b1. Rows past the
-  // end are copies of the last one, halves outside the cache of some other rows.
-  template <bool ONCE>
-  __device__ __forceinline__ void issue(int j0, int b0, int b1, uint32_t lds) const {
-#pragma unroll
-    for (int c = 0; c < COPIES; ++c) {
-      const int half = c * RPC / 16;
-      int j = j0 + 16 * half;
-      const unsigned char* src;
-      int last = rows - 1 - j;  // of the half, counted from its first row
-      if constexpr (PAGED) {
-        const int blk = half ? b1 : b0;
-        // A half without a block is read from block 0; it is not used.
-        src = base + (blk >= 0 ? (size_t)blk : 0) * block_bytes +
-              (size_t)(j & ((1 << shift) - 1)) * T::ROW;
-        last = 15;
-      } else {
-        if (last < 0) {
-          j = rows - 1;
-          last = 0;
-        }
-        src = base + (size_t)j * T::ROW;
+  // Copies the given part of the tile from row j0 on (HALF: its rows 16 HALF .. + 15),
+  // which lies in block blk. Rows past the end are copies of the last one, a half outside
+  // the cache is some other rows.
+  template <int HALF>
+  __device__ __forceinline__ void issue(int j0, int blk, bool once, uint32_t lds) const {
+    int j = j0 + 16 * HALF;
+    const unsigned char* src;
+    int last = rows - 1 - j;  // of the half, counted from its first row
+    if constexpr (PAGED) {
+      // A half without a block is read from block 0; it is not used.
+      src = base + (blk >= 0 ? (size_t)blk : 0) * block_bytes + (size_t)(j & ((1 << shift) - 1)) * T::ROW;
+      last = 15;
+    } else {
+      if (last < 0) {
+        j = rows - 1;
+        last = 0;
       }
+      src = base + (size_t)j * T::ROW;
+    }
+#pragma unroll
+    for (int c = HALF * COPIES / 2; c < (HALF + 1) * COPIES / 2; ++c) {
       const uint32_t off = (uint32_t)(min(c * RPC % 16 + lane_row, last) * T::ROW) + chunk[c];
-      if constexpr (ONCE) copy_to_lds_nt(src, off, lds + c * 1024);
+      if (once) copy_to_lds_nt(src, off, lds + c * 1024);
       else copy_to_lds(src, off, lds + c * 1024);
     }
   }
@@ -88,96 +84,41 @@ __device__ __forceinline__ uint32_t below(int n) {
   return n >= 32 ? ~0u : n > 0 ? (1u << n) - 1 : 0u;
 }
 
-template <int D, int QB, bool CAP, bool BIAS, bool PAGED>
-__global__ __launch_bounds__(kThreads, 2) void tree_kernel(TreeParams p) {
-  constexpr int BQ = 16 * QB, KS = D / 32, DB = D / 16;
+// The query rows of a wave and their running results: rows m0 + 16 qb + fr of the T H / G
+// rows of a (sequence, group), row m being token m / R of head m % R of the group.
+template <int D, int QB, bool CAP, bool BIAS>
+struct TreeRows {
+  static constexpr int KS = D / 32, DB = D / 16;
   using T = AttnTile<D, kTreeTile>;
   using Form = ScoreForm<CAP, BIAS>;
-  constexpr int RING = 2 * T::BYTES;
-  static_assert(RING >= BQ * D * 4, "a wave's results fit its ring");
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  __shared__ float s_ml[NW][BQ][2];
-  __shared__ int s_depth[BIAS ? kMaxDrafts : 1];
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int fr = lane & 15, grp = lane >> 4;
-  const int R = p.H / p.G, M = p.T * R, blocks = (M + BQ - 1) / BQ;
-  const int g = blockIdx.x % p.G, m0 = (int)(blockIdx.x / p.G % blocks) * BQ;
-  const int c = blockIdx.x / p.G / blocks;
-  TreeSpan sp;
-  if (!tree_span(p, lane, c, -1, sp)) return;
-
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
-  const uint32_t ring = lds0 + wave * RING;
-  const CacheTiles<D, PAGED> cp(p, sp, g, lane);
-  auto row0 = [&](int t) { return (sp.tile0 + t) * kTreeTile; };
-  const bool once = blocks == 1;
-  auto issue = [&](int t, int b0, int b1, int stage) {
-    if (once) cp.template issue<true>(row0(t), b0, b1, ring + stage * T::BYTES);
-    else cp.template issue<false>(row0(t), b0, b1, ring + stage * T::BYTES);
-  };
-  // Blocks of the tile at hand (now), the next one, and the one after it, whose table
-  // entries are read a tile ahead of its copies.
-  int now0 = -1, now1 = -1, next0 = -1, next1 = -1;
-  if (wave < sp.tiles) {
-    now0 = cp.block(row0(wave));
-    now1 = cp.block(row0(wave) + 16);
-    next0 = cp.block(row0(wave + NW));
-    next1 = cp.block(row0(wave + NW) + 16);
-    issue(wave, now0, now1, 0);
-  }
-
-  // Query row m0 + 16 qb + fr: token m / R of head m % R of the group.
   bf16x8_t qf[QB][KS];
   uint64_t word[QB];
-  int place[QB];  // its depth
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const int m = min(m0 + qb * 16 + fr, M - 1), t = m / R;
-    const uint16_t* src = static_cast<const uint16_t*>(p.q) +
-                          (((size_t)sp.b * p.T + t) * p.H + g * R + m % R) * D + grp * 8;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      qf[qb][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(src + ks * 32));
-    word[qb] = tree_word(p, sp.b, t);
-    place[qb] = tree_depth(word[qb], t);
-  }
+  int place[QB];    // depth
   float slope[QB];  // in log2 units
-  if constexpr (BIAS) {
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-      slope[qb] = p.slopes[g * R + min(m0 + qb * 16 + fr, M - 1) % R] * kScoredLog2e;
-    for (int t = threadIdx.x; t < p.T; t += kThreads) s_depth[t] = tree_depth(tree_word(p, sp.b, t), t);
-    __syncthreads();
-  }
-  const Form form(p.scale, p.cap);
   f32x4_t o[DB][QB];
   float m[QB], l[QB];
+  __device__ __forceinline__ void load(const TreeParams& p, int b, int g, int R, int M, int m0, int fr, int grp) {
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    m[qb] = -INFINITY;
-    l[qb] = 0.f;
+    for (int qb = 0; qb < QB; ++qb) {
+      const int row = min(m0 + qb * 16 + fr, M - 1), t = row / R, r = row - t * R;
+      const uint16_t* src =
+          static_cast<const uint16_t*>(p.q) + (((size_t)b * p.T + t) * p.H + g * R + r) * D + grp * 8;
 #pragma unroll
-    for (int i = 0; i < DB; ++i) o[i][qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
-  const FragOffsets<D> fo(fr, grp);
-  int stage = 0;
-  for (int t = wave; t < sp.tiles; t += NW) {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the other stage has been read
-    const int j0 = row0(t), b0 = now0, b1 = now1;
-    if (t + NW < sp.tiles) {
-      issue(t + NW, next0, next1, stage ^ 1);
-      now0 = next0;
-      now1 = next1;
-      next0 = cp.block(row0(t + 2 * NW));
-      next1 = cp.block(row0(t + 2 * NW) + 16);
-      KL_WAIT_VMCNT(T::BYTES / 1024);
-    } else {
-      KL_WAIT_VMCNT(0);
+      for (int ks = 0; ks < KS; ++ks)
+        qf[qb][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(src + ks * 32));
+      word[qb] = tree_word(p, b, t);
+      place[qb] = tree_depth(word[qb], t);
+      if constexpr (BIAS) slope[qb] = p.slopes[g * R + r] * kScoredLog2e;
+      m[qb] = -INFINITY;
+      l[qb] = 0.f;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[i][qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    asm volatile("" ::: "memory");
-    const FragOffsets<D> fi = fo.at(ring + stage * T::BYTES);
-    stage ^= 1;
+  }
+  // One landed tile, whose first row is j0 and whose halves end at rows end0 and end1.
+  __device__ __forceinline__ void take(const Form& form, const FragOffsets<D>& fi, const TreeParams& p,
+                                       const TreeSeg& sp, int j0, int end0, int end1, const int* s_depth,
+                                       int grp) {
     f32x4_t sc[2][QB];
     bf16x8_t sa[2][KS];
 #pragma unroll
@@ -192,8 +133,6 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(TreeParams p) {
         for (int qb = 0; qb < QB; ++qb)
           sc[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
               sa[kb][ks], qf[qb][ks], ks == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[kb][qb], 0, 0, 0);
-    // The rows of each half end with the sequence; a half outside the cache has none.
-    const int end0 = PAGED && b0 < 0 ? 0 : sp.rows, end1 = PAGED && b1 < 0 ? 0 : sp.rows;
     const bool edge = j0 + kTreeTile > min(sp.n, min(end0, end1));
     const int jl = j0 + grp * 4;
     // Bit i: this lane's query sees row j0 + 4 grp + i.
@@ -230,32 +169,163 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(TreeParams p) {
       for (int qb = 0; qb < QB; ++qb)
         o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[db], pf[qb], o[db][qb], 0, 0, 0);
   }
+};
 
-  WaveMerge<D, QB, NW> merge(s_ml, lds0, RING, wave, fr, grp);
-  merge.put(m, l, o);
-  for (int e = threadIdx.x; e < BQ * D / 4; e += kThreads) {
-    const int row = e / (D / 4), piece = e % (D / 4), mr = m0 + row;
-    if (mr >= M) continue;
-    float mm, sum;
-    const f32x4_t x = merge.get(row, piece, mm, sum);
-    if (sp.S == 1) {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      uint16_t* dst = static_cast<uint16_t*>(p.out) +
-                      (((size_t)sp.b * p.T + mr / R) * p.H + g * R + mr % R) * D + piece * 4;
-      *reinterpret_cast<u32x2*>(dst) = u32x2{pack2(x[0] * inv, x[1] * inv), pack2(x[2] * inv, x[3] * inv)};
-    } else {
-      *reinterpret_cast<f32x4_t*>(tree_part(p, c, g, mr) + piece * 4) = x;
-      if (piece == 0) {
-        float* ml = tree_part_ml(p, c, g, mr);
-        ml[0] = mm;
-        ml[1] = sum;
-      }
+// Stores four columns of a merged row: the output where the segment is the whole
+// sequence, else the slot's partial result.
+template <int D>
+__device__ __forceinline__ void tree_store(const TreeParams& p, const TreeSeg& sp, int g, int R, int mr, int piece,
+                                           f32x4_t x, float mm, float sum) {
+  if (sp.whole) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int t = mr / R;
+    uint16_t* dst =
+        static_cast<uint16_t*>(p.out) + (((size_t)sp.b * p.T + t) * p.H + g * R + mr - t * R) * D + piece * 4;
+    *reinterpret_cast<u32x2*>(dst) = u32x2{pack2(x[0] * inv, x[1] * inv), pack2(x[2] * inv, x[3] * inv)};
+  } else {
+    *reinterpret_cast<f32x4_t*>(tree_part(p, sp.slot, g, mr) + piece * 4) = x;
+    if (piece == 0) {
+      float* ml = tree_part_ml(p, sp.slot, g, mr);
+      ml[0] = mm;
+      ml[1] = sum;
     }
   }
 }
 
-// Joins the chunks of a sequence, in chunk order: SUB lanes groups of D / 4 lanes per
-// row, each taking every SUB-th chunk, added in a fixed order.
+// NB blocks of 16 QB query rows per workgroup, four waves each. The four waves of a block
+// share a segment's 32-row tiles, tile t to wave t % 4. With one block a wave's tiles come
+// through a private two-stage ring with no barrier. With two, the waves of both blocks
+// work on the same four tiles at a time, each wave having copied one half tile, through
+// four common stages with one barrier per four tiles: a cached row is copied once for all
+// 32 QB rows, where two workgroups of one block each copied it twice (16 x 16 tokens, 32
+// heads on 8 groups, 1k to 32k rows: 111 us, 66 with half the tokens).
+template <int D, int QB, int NB, bool CAP, bool BIAS, bool PAGED>
+__global__ __launch_bounds__(NB * 256, NB == 1 ? 2 : 1) void tree_kernel(TreeParams p) {
+  constexpr int BQ = 16 * QB;
+  using T = AttnTile<D, kTreeTile>;
+  constexpr int STAGES = NB == 1 ? 2 : 4;
+  constexpr int RESULT = BQ * D * 4;  // a wave's results
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ float s_ml[NB][NW][BQ][2];
+  __shared__ int s_depth[BIAS ? kMaxDrafts : 1];
+  const int lane = threadIdx.x & 63;
+  const int wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = wave8 % NW, rb = wave8 / NW;
+  const int fr = lane & 15, grp = lane >> 4;
+  const int R = p.H / p.G, M = p.T * R, blocks = (M + NB * BQ - 1) / (NB * BQ);
+  const int g = blockIdx.x % p.G, w0 = (int)(blockIdx.x / p.G % blocks) * (NB * BQ), m0 = w0 + rb * BQ;
+  const int c = blockIdx.x / p.G / blocks;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
+  const bool once = blocks == 1;
+  const ScoreForm<CAP, BIAS> form(p.scale, p.cap);
+  const FragOffsets<D> fo(fr, grp);
+  TreeWalk walk(p, lane, c);
+  TreeSeg sp;
+  while (walk.next(p, lane, sp)) {
+    const CacheTiles<D, PAGED> cp(p, sp, g, lane);
+    auto row0 = [&](int t) { return (sp.tile0 + t) * kTreeTile; };
+    auto end_of = [&](int blk) { return PAGED && blk < 0 ? 0 : sp.rows; };
+    TreeRows<D, QB, CAP, BIAS> rows;
+    if constexpr (NB == 1) {
+      const uint32_t ring = lds0 + wave * (2 * T::BYTES);
+      auto issue = [&](int t, int b0, int b1, int stage) {
+        cp.template issue<0>(row0(t), b0, once, ring + stage * T::BYTES);
+        cp.template issue<1>(row0(t), b1, once, ring + stage * T::BYTES);
+      };
+      // Blocks of the tile at hand and of the next one, read a tile ahead of its copies.
+      int now0 = -1, now1 = -1, next0 = -1, next1 = -1;
+      if (wave < sp.tiles) {
+        now0 = cp.block(row0(wave));
+        now1 = cp.block(row0(wave) + 16);
+        next0 = cp.block(row0(wave + NW));
+        next1 = cp.block(row0(wave + NW) + 16);
+        issue(wave, now0, now1, 0);
+      }
+      rows.load(p, sp.b, g, R, M, m0, fr, grp);
+      if constexpr (BIAS) {
+        for (int t = threadIdx.x; t < p.T; t += NB * 256) s_depth[t] = tree_depth(tree_word(p, sp.b, t), t);
+        __syncthreads();
+      }
+      int stage = 0;
+      for (int t = wave; t < sp.tiles; t += NW) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the other stage has been read
+        const int b0 = now0, b1 = now1;
+        if (t + NW < sp.tiles) {
+          issue(t + NW, next0, next1, stage ^ 1);
+          now0 = next0;
+          now1 = next1;
+          next0 = cp.block(row0(t + 2 * NW));
+          next1 = cp.block(row0(t + 2 * NW) + 16);
+          KL_WAIT_VMCNT(T::BYTES / 1024);
+        } else {
+          KL_WAIT_VMCNT(0);
+        }
+        asm volatile("" ::: "memory");
+        rows.take(form, fo.at(ring + stage * T::BYTES), p, sp, row0(t), end_of(b0), end_of(b1), s_depth, grp);
+        stage ^= 1;
+      }
+    } else {
+      // Step i takes tiles 4 i .. 4 i + 3 from stage i % 4; this wave copies half rb of
+      // tile 4 i + wave and takes that tile.
+      constexpr int AHEAD = STAGES - 1, COPIES = T::BYTES / 2048;
+      const int steps = (sp.tiles + NW - 1) / NW;
+      int blk[AHEAD + 1][2];  // blocks of the halves of this wave's tiles of steps i .. i + 3
+      auto look = [&](int i, int (&x)[2]) {
+        x[0] = cp.block(row0(NW * i + wave));
+        x[1] = cp.block(row0(NW * i + wave) + 16);
+      };
+      auto issue = [&](int i, const int (&x)[2]) {
+        const int t = NW * i + wave;
+        const uint32_t at = lds0 + ((i % STAGES) * NW + wave) * T::BYTES;
+        // A step's last tiles may not exist: their rows are copies of the last one.
+        if (rb == 0) cp.template issue<0>(row0(t), x[0], once, at);
+        else cp.template issue<1>(row0(t), x[1], once, at);
+      };
+#pragma unroll
+      for (int i = 0; i <= AHEAD; ++i) look(i, blk[i]);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (i < steps) issue(i, blk[i]);
+      rows.load(p, sp.b, g, R, M, m0, fr, grp);
+      if constexpr (BIAS)
+        for (int t = threadIdx.x; t < p.T; t += NB * 256) s_depth[t] = tree_depth(tree_word(p, sp.b, t), t);
+      KL_WAIT_VMCNT(0);
+      for (int i = 0; i < steps; ++i) {
+        const int ahead = min(AHEAD - 1, steps - 1 - i);  // steps issued after this one
+        if (ahead == 2) KL_WAIT_VMCNT(2 * COPIES);
+        else if (ahead == 1) KL_WAIT_VMCNT(COPIES);
+        else KL_WAIT_VMCNT(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage refilled below has been read
+        __syncthreads();
+        if (i + AHEAD < steps) issue(i + AHEAD, blk[AHEAD]);
+        const int t = NW * i + wave, b0 = blk[0][0], b1 = blk[0][1];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+          blk[k][0] = blk[k + 1][0];
+          blk[k][1] = blk[k + 1][1];
+        }
+        look(i + AHEAD + 1, blk[AHEAD]);
+        if (t < sp.tiles)
+          rows.take(form, fo.at(lds0 + ((i % STAGES) * NW + wave) * T::BYTES), p, sp, row0(t), end_of(b0),
+                    end_of(b1), s_depth, grp);
+      }
+    }
+    WaveMerge<D, QB, NW> merge(s_ml[rb], lds0 + rb * NW * RESULT, RESULT, wave, fr, grp);
+    merge.put(rows.m, rows.l, rows.o);
+    for (int e = threadIdx.x; e < NB * BQ * D / 4; e += NB * 256) {
+      const int row = e / (D / 4), piece = e % (D / 4), mr = w0 + row, k = row / BQ;
+      if (mr >= M) continue;
+      const WaveMerge<D, QB, NW> from(s_ml[k], lds0 + k * NW * RESULT, RESULT, wave, fr, grp);
+      float mm, sum;
+      const f32x4_t x = from.get(row - k * BQ, piece, mm, sum);
+      tree_store<D>(p, sp, g, R, mr, piece, x, mm, sum);
+    }
+    __syncthreads();  // the results have been read: the next segment may fill their place
+  }
+}
+
+// Joins a sequence's partial results, in slot order: SUB groups of D / 4 lanes per row,
+// each taking every SUB-th slot, added in a fixed order.
 template <typename E, int D, int SUB>
 __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeParams p) {
   constexpr int LANES = D / 4, ROWS = kThreads / LANES / SUB;  // rows per workgroup
@@ -266,8 +336,9 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeParams p) {
   const int g = blockIdx.x % p.G, b = blockIdx.x / p.G / blocks;
   const int slot = threadIdx.x / LANES, piece = threadIdx.x % LANES, sub = slot % SUB;
   const int row = (int)(blockIdx.x / p.G % blocks) * ROWS + slot / SUB, m = min(row, M - 1);
-  TreeSpan sp;
-  if (!tree_span(p, lane, 0, b, sp) || sp.S == 1) return;
+  int first;
+  const int count = tree_slots(p, lane, b, first);
+  if (count == 1) return;
   float mm = -INFINITY, sum = 0.f;
   f32x4_t x = {0.f, 0.f, 0.f, 0.f};
   auto take = [&](float mk, float lk, f32x4_t xk) {
@@ -278,9 +349,9 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeParams p) {
     x = x * f + xk * fk;
   };
 #pragma unroll 4
-  for (int s = sub; s < sp.S; s += SUB) {
-    const float* ml = tree_part_ml(p, sp.first + s, g, m);
-    take(ml[0], ml[1], *reinterpret_cast<const f32x4_t*>(tree_part(p, sp.first + s, g, m) + piece * 4));
+  for (int s = sub; s < count; s += SUB) {
+    const float* ml = tree_part_ml(p, first + s, g, m);
+    take(ml[0], ml[1], *reinterpret_cast<const f32x4_t*>(tree_part(p, first + s, g, m) + piece * 4));
   }
   if constexpr (SUB > 1) {
     s_x[threadIdx.x] = x;
@@ -303,20 +374,28 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeParams p) {
     *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + at) = x * inv;
 }
 
-template <int D, int QB, bool CAP, bool BIAS, bool PAGED>
+template <int D, int QB, int NB, bool CAP, bool BIAS, bool PAGED>
 hipError_t launch_tree(const TreeParams& p, hipStream_t st) {
-  constexpr int lds = NW * 2 * AttnTile<D, kTreeTile>::BYTES;
-  const unsigned blocks = (p.T * (p.H / p.G) + 16 * QB - 1) / (16 * QB);
-  hipLaunchKernelGGL((tree_kernel<D, QB, CAP, BIAS, PAGED>), dim3((p.chunks + p.B) * blocks * p.G),
-                     dim3(kThreads), lds, st, p);
+  constexpr int tile = AttnTile<D, kTreeTile>::BYTES;
+  constexpr int results = NB * NW * 16 * QB * D * 4, stages = NB == 1 ? NW * 2 * tile : NW * 4 * tile;
+  constexpr int lds = results > stages ? results : stages;
+  const unsigned blocks = (p.T * (p.H / p.G) + 16 * QB * NB - 1) / (16 * QB * NB);
+  if (lds > 65536) {
+    static std::atomic<uint32_t> done{0};
+    const hipError_t e =
+        set_max_lds(reinterpret_cast<const void*>(tree_kernel<D, QB, NB, CAP, BIAS, PAGED>), lds, done);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((tree_kernel<D, QB, NB, CAP, BIAS, PAGED>),
+                     dim3((unsigned)p.chunks * (p.per > 0 ? p.B : 1) * blocks * p.G), dim3(NB * 256), lds, st, p);
   return hipGetLastError();
 }
 
-template <int D, int QB>
+template <int D, int QB, int NB>
 hipError_t launch_qb(const TreeParams& p, hipStream_t st) {
   auto layout = [&](auto cap, auto bias) {
-    return p.paged ? launch_tree<D, QB, decltype(cap)::value, decltype(bias)::value, true>(p, st)
-                   : launch_tree<D, QB, decltype(cap)::value, decltype(bias)::value, false>(p, st);
+    return p.paged ? launch_tree<D, QB, NB, decltype(cap)::value, decltype(bias)::value, true>(p, st)
+                   : launch_tree<D, QB, NB, decltype(cap)::value, decltype(bias)::value, false>(p, st);
   };
   using Y = std::true_type;
   using N = std::false_type;
@@ -342,7 +421,9 @@ hipError_t launch_merge(const TreeParams& p, hipStream_t st) {
 
 template <int D>
 hipError_t launch_d(const TreeParams& p, hipStream_t st) {
-  const hipError_t e = p.T * (p.H / p.G) <= 16 ? launch_qb<D, 1>(p, st) : launch_qb<D, 2>(p, st);
+  const hipError_t e = p.block_rows == 16   ? launch_qb<D, 1, 1>(p, st)
+                       : p.block_rows == 32 ? launch_qb<D, 2, 1>(p, st)
+                                            : launch_qb<D, 2, 2>(p, st);
   return e != hipSuccess || !p.part ? e : launch_tree_merge(p, st);
 }
 

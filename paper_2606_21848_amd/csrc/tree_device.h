@@ -1,8 +1,12 @@
 // The work split of the drafted-token decode, which its kernels derive from the lengths
-// on the device: the rows of every sequence (cached and drafted) are cut into chunks of
-// `per` 32-row tiles, chunk after chunk and sequence after sequence. A sequence of one
-// chunk is written by the workgroups that hold it; the others leave partial results that
-// a merge kernel joins in chunk order.
+// on the device. A sequence's rows, cached and drafted, are 32-row tiles.
+//  - Shared (p.per == 0): the tiles of all sequences, one after another, are cut into
+//    p.chunks even pieces, whatever the spread of lengths; a workgroup walks its piece
+//    sequence by sequence.
+//  - Fixed (p.per > 0, few sequences): piece s of p.chunks pieces of each sequence is its
+//    tiles from s p.per on; nothing has to be summed first.
+// A sequence inside one piece is written by its workgroups; the others leave partial
+// results in slots of their own that a merge kernel joins in order.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -13,27 +17,19 @@ namespace kl {
 
 constexpr int kTreeTile = 32;  // rows per tile
 
-struct TreeSpan {
-  int b, s, S;     // sequence, chunk of it, its chunks
-  int first;       // its first chunk among all
-  int n, rows;     // rows cached before the draft, rows in all
-  int tile0, tiles;
-};
-
+__device__ __forceinline__ int tree_capacity(const TreeParams& p) {
+  return p.paged ? p.max_blocks << p.block_shift : p.L_max;
+}
+// Rows cached before the draft, and rows in all.
 __device__ __forceinline__ int tree_cached(const TreeParams& p, int b) {
-  const int cap = p.paged ? p.max_blocks << p.block_shift : p.L_max;
-  return min(max(((const __attribute__((address_space(4))) int*)p.lengths)[b], 0), cap);
+  return min(max(((const __attribute__((address_space(4))) int*)p.lengths)[b], 0), tree_capacity(p));
 }
-__device__ __forceinline__ int tree_rows(const TreeParams& p, int n) {
-  const int cap = p.paged ? p.max_blocks << p.block_shift : p.L_max;
-  return min(n + p.T, cap);
-}
+__device__ __forceinline__ int tree_rows(const TreeParams& p, int n) { return min(n + p.T, tree_capacity(p)); }
+// Tiles of a sequence: one at least, whose workgroups write its zero rows.
+__device__ __forceinline__ int tree_tiles(int rows) { return max((rows + kTreeTile - 1) / kTreeTile, 1); }
 __device__ __forceinline__ int tree_lane_tiles(const TreeParams& p, int b) {
   if (b >= p.B) return 0;
-  const int cap = p.paged ? p.max_blocks << p.block_shift : p.L_max;
-  const int n = min(max(p.lengths[b], 0), cap);
-  // A sequence has one chunk at least, whose workgroups write its zero rows.
-  return max((tree_rows(p, n) + kTreeTile - 1) / kTreeTile, 1);
+  return tree_tiles(tree_rows(p, min(max(p.lengths[b], 0), tree_capacity(p))));
 }
 
 __device__ __forceinline__ long wave_sum(long x) {
@@ -41,64 +37,101 @@ __device__ __forceinline__ long wave_sum(long x) {
   for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
   return x;
 }
-__device__ __forceinline__ int wave_sum(int x) {
+__device__ __forceinline__ int wave_prefix(int x, int lane) {  // inclusive
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    x += lane >= o ? y : 0;
+  }
   return x;
 }
 
-// Tiles per chunk: the fewest that give at most p.chunks chunks, and p.least at least
-// (with more than 64 sequences, or not many fewer than chunks, an even share of all
-// tiles, which gives at most B chunks more).
-__device__ __forceinline__ int tree_per(const TreeParams& p, int lane) {
-  long total = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) total += wave_sum((long)tree_lane_tiles(p, b0 + lane));
-  int per = max((int)((total + p.chunks - 1) / p.chunks), p.least);
-  if (p.B <= 64 && 2 * p.B <= p.chunks) {
-    const int n = tree_lane_tiles(p, lane);
-    int fits = 2 * per;  // sum ceil(n / 2 per) <= chunks / 2 + B
-    int lo = per;
-    while (lo < fits) {
-      const int mid = (lo + fits) / 2;
-      if (wave_sum((n + mid - 1) / mid) <= p.chunks) fits = mid;
-      else lo = mid + 1;
-    }
-    per = fits;
-  }
-  return __builtin_amdgcn_readfirstlane(per);
+// Tiles per piece of the shared split (all of them are fewer than 2^31).
+__device__ __forceinline__ int tree_share(const TreeParams& p, int lane, int& total) {
+  long sum = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) sum += wave_sum((long)tree_lane_tiles(p, b0 + lane));
+  total = __builtin_amdgcn_readfirstlane((int)sum);
+  return max((total + p.chunks - 1) / p.chunks, p.least);
 }
 
-// The chunk `c` of all (want_b < 0), or the first chunk of sequence want_b; false when
-// there are not that many. Uniform over the wave.
-__device__ __forceinline__ bool tree_span(const TreeParams& p, int lane, int c, int want_b, TreeSpan& t) {
-  const int per = tree_per(p, lane);
-  int before = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) {
-    const int S = (tree_lane_tiles(p, b0 + lane) + per - 1) / per;
-    int pre = S;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(pre, o);
-      if (lane >= o) pre += x;
+struct TreeSeg {
+  int b, n, rows;     // sequence, rows cached before its draft, rows in all
+  int tile0, tiles;   // the piece's tiles of it
+  int slot;           // where partial results go
+  bool whole;         // all of its tiles
+};
+
+// The segments of piece c; uniform over the wave.
+struct TreeWalk {
+  int c, b, b0, tiles_of_lane, off, left;
+  __device__ __forceinline__ TreeWalk(const TreeParams& p, int lane, int c_) : c(c_), b(0), b0(0), off(0) {
+    if (p.per > 0) {
+      b = c / p.chunks;
+      left = 1;
+      return;
     }
-    const int all = __builtin_amdgcn_readlane(pre, 63);
-    const uint64_t hit = want_b < 0 ? __builtin_amdgcn_ballot_w64(before + pre > c)
-                                    : (want_b < b0 + 64 ? 1ull << (want_b - b0) : 0);
-    if (hit) {
-      const int at = __builtin_ctzll(hit);
-      t.b = b0 + at;
-      t.S = __builtin_amdgcn_readlane(S, at);
-      t.first = before + __builtin_amdgcn_readlane(pre, at) - t.S;
-      t.s = want_b < 0 ? c - t.first : 0;
-      t.n = tree_cached(p, t.b);
-      t.rows = tree_rows(p, t.n);
-      t.tile0 = t.s * per;
-      t.tiles = min((t.rows + kTreeTile - 1) / kTreeTile - t.tile0, per);
+    int total;
+    const int per = tree_share(p, lane, total), from = c * per;
+    left = min(per, total - from);
+    if (left <= 0) return;
+    int before = 0;
+    for (;; b0 += 64) {
+      tiles_of_lane = tree_lane_tiles(p, b0 + lane);
+      const int pre = wave_prefix(tiles_of_lane, lane);
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(before + pre > from);
+      if (hit) {
+        const int at = __builtin_ctzll(hit);
+        b = b0 + at;
+        off = from - (before + __builtin_amdgcn_readlane(pre, at) - __builtin_amdgcn_readlane(tiles_of_lane, at));
+        return;
+      }
+      before += __builtin_amdgcn_readlane(pre, 63);
+    }
+  }
+  __device__ __forceinline__ bool next(const TreeParams& p, int lane, TreeSeg& s) {
+    if (left <= 0) return false;
+    s.b = b;
+    s.n = tree_cached(p, b);
+    s.rows = tree_rows(p, s.n);
+    const int real = (s.rows + kTreeTile - 1) / kTreeTile;
+    if (p.per > 0) {
+      left = 0;
+      s.tile0 = (c - b * p.chunks) * p.per;
+      if (s.tile0 > 0 && s.tile0 >= real) return false;
+      s.tiles = min(real - s.tile0, p.per);
+      s.whole = real <= p.per;
+      s.slot = c;
       return true;
     }
-    before += all;
+    const int all = __builtin_amdgcn_readlane(tiles_of_lane, b - b0), take = min(all - off, left);
+    s.tile0 = off;
+    s.tiles = min(real - off, take);
+    s.whole = take == all;
+    s.slot = c + b;  // along the pieces c and b never fall, and one of them grows
+    left -= take;
+    off = 0;
+    if (++b == b0 + 64) {
+      b0 += 64;
+      tiles_of_lane = tree_lane_tiles(p, b0 + lane);
+    }
+    return true;
   }
-  return false;
+};
+
+// The slots that hold sequence b's partial results: `count` from `first` on; one when the
+// sequence was written directly.
+__device__ __forceinline__ int tree_slots(const TreeParams& p, int lane, int b, int& first) {
+  if (p.per > 0) {
+    first = b * p.chunks;
+    return (tree_tiles(tree_rows(p, tree_cached(p, b))) + p.per - 1) / p.per;
+  }
+  int total, before = 0, b0 = 0;
+  const int per = tree_share(p, lane, total);
+  for (; b0 + 64 <= b; b0 += 64) before += (int)wave_sum((long)tree_lane_tiles(p, b0 + lane));
+  const int n = tree_lane_tiles(p, b0 + lane), pre = wave_prefix(n, lane);
+  const int end = before + __builtin_amdgcn_readlane(pre, b - b0), from = end - __builtin_amdgcn_readlane(n, b - b0);
+  first = from / per + b;
+  return (end - 1) / per - from / per + 1;
 }
 
 // What drafted token t sees of the draft, as a word without bits past T; its depth.
@@ -108,8 +141,8 @@ __device__ __forceinline__ uint64_t tree_word(const TreeParams& p, int b, int t)
 }
 __device__ __forceinline__ int tree_depth(uint64_t word, int t) { return __popcll(word & ~(1ull << t)); }
 
-// Where chunk c leaves row m of group g: its weighted sums [D], and its reference (log2
-// units) and weight sum.
+// Row m of group g in slot c: its weighted sums [D], and its reference (log2 units) and
+// weight sum.
 __device__ __forceinline__ float* tree_part(const TreeParams& p, int c, int g, int m) {
   return p.part + (((size_t)c * p.G + g) * p.T * (p.H / p.G) + m) * p.D;
 }
