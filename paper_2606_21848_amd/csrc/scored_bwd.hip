@@ -73,10 +73,10 @@ __device__ __forceinline__ SeenBounds seen_by_rows(const ScoredParams& p, int b,
       p.row_hi[(size_t)b * p.N + q] = seen[qb].hi;
     }
   }
-  sb.over_lanes(15);
+  sb.over_rows();
   sb.make_uniform();
   if (publish && q0 < p.N) {
-    pub.over_lanes(15);
+    pub.over_rows();
     if (fr == 0 && grp == 0)
       static_cast<i32x4*>(p.tile_sees)[(size_t)b * ((p.N + 31) / 32) + q0 / 32] =
           i32x4{pub.any_lo, pub.any_hi, pub.all_lo, pub.all_hi};
@@ -409,10 +409,8 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
       last = max(last, t + 1);
     }
   }
-  for (int o = 1; o < 64; o <<= 1) {
-    first = min(first, __shfl_xor(first, o));
-    last = max(last, __shfl_xor(last, o));
-  }
+  first = wave_reduce(first, [](int x, int y) { return min(x, y); });
+  last = wave_reduce(last, [](int x, int y) { return max(x, y); });
   if (lane == 0) {
     s_first[wave] = first;
     s_last[wave] = last;

@@ -13,6 +13,30 @@ namespace kl {
 constexpr float kScoredLog2e = 1.4426950408889634f;
 constexpr float kScoredLn2 = 0.69314718055994531f;
 
+// Lane permutation within rows of 16 lanes; lanes without a source get `none`.
+template <int CTRL>
+__device__ __forceinline__ int dpp_i32(int x, int none = 0) {
+  return __builtin_amdgcn_update_dpp(none, x, CTRL, 0xF, 0xF, false);
+}
+
+// op over each row of 16 lanes (swapped neighbours, pairs, mirrored halves and rows); all
+// of them get the result.
+template <class Op>
+__device__ __forceinline__ int row_reduce(int x, Op op) {
+  x = op(x, dpp_i32<0xB1>(x));
+  x = op(x, dpp_i32<0x4E>(x));
+  x = op(x, dpp_i32<0x141>(x));
+  return op(x, dpp_i32<0x140>(x));
+}
+
+// op over the wave, uniform.
+template <class Op>
+__device__ __forceinline__ int wave_reduce(int x, Op op) {
+  x = row_reduce(x, op);
+  return op(op(__builtin_amdgcn_readlane(x, 0), __builtin_amdgcn_readlane(x, 16)),
+            op(__builtin_amdgcn_readlane(x, 32), __builtin_amdgcn_readlane(x, 48)));
+}
+
 // The value rows [lo, hi) that query row i sees, within [0, N); an empty range is {0, 0}.
 struct SeenRange {
   int lo, hi;
@@ -37,15 +61,12 @@ struct SeenBounds {
     all_lo = max(all_lo, s.lo);
     all_hi = min(all_hi, s.hi);
   }
-  // Over the lanes that differ in the bits of `mask`; all of them get the result.
-  __device__ __forceinline__ void over_lanes(int mask) {
-    for (int o = 1; o <= mask; o <<= 1) {
-      if (!(o & mask)) continue;
-      any_lo = min(any_lo, __shfl_xor(any_lo, o));
-      any_hi = max(any_hi, __shfl_xor(any_hi, o));
-      all_lo = max(all_lo, __shfl_xor(all_lo, o));
-      all_hi = min(all_hi, __shfl_xor(all_hi, o));
-    }
+  // Over each row of 16 lanes; all of them get the result.
+  __device__ __forceinline__ void over_rows() {
+    any_lo = row_reduce(any_lo, [](int a, int b) { return min(a, b); });
+    any_hi = row_reduce(any_hi, [](int a, int b) { return max(a, b); });
+    all_lo = row_reduce(all_lo, [](int a, int b) { return max(a, b); });
+    all_hi = row_reduce(all_hi, [](int a, int b) { return min(a, b); });
   }
   // The same in scalar registers, once every lane holds the same.
   __device__ __forceinline__ void make_uniform() {

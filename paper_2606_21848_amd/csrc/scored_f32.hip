@@ -122,7 +122,7 @@ __global__ __launch_bounds__(NW * 64, 2) void forward_kernel(ScoredParams p) {
   const SeenRange seen = seen_range(p, b, min(q0 + r, p.N - 1));
   SeenBounds sb;
   sb.add(seen);
-  sb.over_lanes(15);
+  sb.over_rows();
   sb.make_uniform();
   const bool any = sb.any_lo < sb.any_hi;
   const int t0 = any ? sb.any_lo / 16 : 0, nblk = any ? (sb.any_hi + 15) / 16 : 0;
@@ -180,8 +180,8 @@ __global__ __launch_bounds__(NW * 64, 2) void dq_kernel(ScoredParams p) {
   SeenBounds sb, pub;
   sb.add(seen);
   pub.add(q0 + r < p.N ? seen : SeenRange{0, 0});
-  sb.over_lanes(15);
-  pub.over_lanes(15);
+  sb.over_rows();
+  pub.over_rows();
   sb.make_uniform();
   if (h == 0 && threadIdx.x < 16) {
     if (q0 + r < p.N) {
@@ -272,10 +272,8 @@ __global__ __launch_bounds__(NW * 64, 2) void dv_kernel(ScoredParams p) {
       last = max(last, t + 1);
     }
   }
-  for (int o = 1; o < 64; o <<= 1) {
-    first = min(first, __shfl_xor(first, o));
-    last = max(last, __shfl_xor(last, o));
-  }
+  first = wave_reduce(first, [](int x, int y) { return min(x, y); });
+  last = wave_reduce(last, [](int x, int y) { return max(x, y); });
   if (lane == 0) {
     s_first[wave] = first;
     s_last[wave] = last;

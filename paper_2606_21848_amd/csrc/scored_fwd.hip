@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p)
     seen[qb] = seen_range(p, b, min(q0 + qb * 16 + fr, p.N - 1));
     sb.add(seen[qb]);
   }
-  sb.over_lanes(15);
+  sb.over_rows();
   sb.make_uniform();
   if (q0 >= p.N) sb.any_lo = sb.any_hi = 0;  // rows past the end: this wave only copies
   if (lane == 0) {
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_split_kernel(ScoredPar
     seen[qb] = seen_range(p, b, min(q0 + qb * 16 + fr, p.N - 1));
     sb.add(seen[qb]);
   }
-  sb.over_lanes(15);
+  sb.over_rows();
   sb.make_uniform();
   const bool any = sb.any_lo < sb.any_hi;
   const int t0 = any ? sb.any_lo / RV : 0, tend = any ? (sb.any_hi + RV - 1) / RV : 0;

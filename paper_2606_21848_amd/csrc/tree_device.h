@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 
 #include "kl_internal.h"
+#include "scored_device.h"
 
 namespace kl {
 
@@ -32,25 +33,23 @@ __device__ __forceinline__ int tree_lane_tiles(const TreeParams& p, int b) {
   return tree_tiles(tree_rows(p, min(max(p.lengths[b], 0), tree_capacity(p))));
 }
 
-__device__ __forceinline__ long wave_sum(long x) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
-  return x;
+__device__ __forceinline__ int wave_sum(int x) {  // uniform
+  return wave_reduce(x, [](int a, int b) { return a + b; });
 }
 __device__ __forceinline__ int wave_prefix(int x, int lane) {  // inclusive
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o);
-    x += lane >= o ? y : 0;
-  }
-  return x;
+  x += dpp_i32<0x111>(x);  // by 1, 2, 4 and 8 lanes within rows of 16
+  x += dpp_i32<0x112>(x);
+  x += dpp_i32<0x114>(x);
+  x += dpp_i32<0x118>(x);
+  const int a = __builtin_amdgcn_readlane(x, 15), b = a + __builtin_amdgcn_readlane(x, 31),
+            c = b + __builtin_amdgcn_readlane(x, 47);
+  return x + (lane < 16 ? 0 : lane < 32 ? a : lane < 48 ? b : c);
 }
 
 // Tiles per piece of the shared split (all of them are fewer than 2^31).
 __device__ __forceinline__ int tree_share(const TreeParams& p, int lane, int& total) {
-  long sum = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) sum += wave_sum((long)tree_lane_tiles(p, b0 + lane));
-  total = __builtin_amdgcn_readfirstlane((int)sum);
+  total = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) total += wave_sum(tree_lane_tiles(p, b0 + lane));
   return max((total + p.chunks - 1) / p.chunks, p.least);
 }
 
@@ -127,7 +126,7 @@ __device__ __forceinline__ int tree_slots(const TreeParams& p, int lane, int b, 
   }
   int total, before = 0, b0 = 0;
   const int per = tree_share(p, lane, total);
-  for (; b0 + 64 <= b; b0 += 64) before += (int)wave_sum((long)tree_lane_tiles(p, b0 + lane));
+  for (; b0 + 64 <= b; b0 += 64) before += wave_sum(tree_lane_tiles(p, b0 + lane));
   const int n = tree_lane_tiles(p, b0 + lane), pre = wave_prefix(n, lane);
   const int end = before + __builtin_amdgcn_readlane(pre, b - b0), from = end - __builtin_amdgcn_readlane(n, b - b0);
   first = from / per + b;
