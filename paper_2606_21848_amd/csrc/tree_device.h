@@ -46,11 +46,34 @@ __device__ __forceinline__ int wave_prefix(int x, int lane) {  // inclusive
   return x + (lane < 16 ? 0 : lane < 32 ? a : lane < 48 ? b : c);
 }
 
-// Tiles per piece of the shared split (all of them are fewer than 2^31).
-__device__ __forceinline__ int tree_share(const TreeParams& p, int lane, int& total) {
-  total = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) total += wave_sum(tree_lane_tiles(p, b0 + lane));
-  return max((total + p.chunks - 1) / p.chunks, p.least);
+// The shared split: tiles per piece, and whether every sequence starts a piece of its own.
+// A workgroup's second sequence costs it the latencies of a start and a merge, some 5 us,
+// the time of a dozen tiles: short pieces are kept apart (6 sequences of 5 to 1500 rows,
+// fp32: 15.8 us across them, 12.6 apart).
+struct TreeShare {
+  int per, total;
+  bool apart;
+  // Tiles of a sequence of n, with the idle ones behind it that end its last piece.
+  __device__ __forceinline__ int padded(int n) const { return apart ? (n + per - 1) / per * per : n; }
+};
+constexpr int kShortPiece = 16;
+__device__ __forceinline__ TreeShare tree_share(const TreeParams& p, int lane) {
+  TreeShare s;
+  s.total = 0;
+  int n = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) {
+    n = tree_lane_tiles(p, b0 + lane);
+    s.total += wave_sum(n);
+  }
+  s.per = max((s.total + p.chunks - 1) / p.chunks, p.least);
+  s.apart = p.B <= 64 && 2 * p.B <= p.chunks && s.per <= kShortPiece;
+  if (s.apart) {
+    // At twice the even share there are at most chunks / 2 + B pieces: this ends.
+    int pieces = wave_sum((n + s.per - 1) / s.per);
+    while (pieces > p.chunks) pieces = wave_sum((n + ++s.per - 1) / s.per);
+    s.total = pieces * s.per;
+  }
+  return s;
 }
 
 struct TreeSeg {
@@ -63,19 +86,20 @@ struct TreeSeg {
 // The segments of piece c; uniform over the wave.
 struct TreeWalk {
   int c, b, b0, tiles_of_lane, off, left;
+  TreeShare share;
   __device__ __forceinline__ TreeWalk(const TreeParams& p, int lane, int c_) : c(c_), b(0), b0(0), off(0) {
     if (p.per > 0) {
       b = c / p.chunks;
       left = 1;
       return;
     }
-    int total;
-    const int per = tree_share(p, lane, total), from = c * per;
-    left = min(per, total - from);
+    share = tree_share(p, lane);
+    const int from = c * share.per;
+    left = min(share.per, share.total - from);
     if (left <= 0) return;
     int before = 0;
     for (;; b0 += 64) {
-      tiles_of_lane = tree_lane_tiles(p, b0 + lane);
+      tiles_of_lane = share.padded(tree_lane_tiles(p, b0 + lane));
       const int pre = wave_prefix(tiles_of_lane, lane);
       const uint64_t hit = __builtin_amdgcn_ballot_w64(before + pre > from);
       if (hit) {
@@ -111,7 +135,7 @@ struct TreeWalk {
     off = 0;
     if (++b == b0 + 64) {
       b0 += 64;
-      tiles_of_lane = tree_lane_tiles(p, b0 + lane);
+      tiles_of_lane = share.padded(tree_lane_tiles(p, b0 + lane));
     }
     return true;
   }
@@ -124,10 +148,11 @@ __device__ __forceinline__ int tree_slots(const TreeParams& p, int lane, int b, 
     first = b * p.chunks;
     return (tree_tiles(tree_rows(p, tree_cached(p, b))) + p.per - 1) / p.per;
   }
-  int total, before = 0, b0 = 0;
-  const int per = tree_share(p, lane, total);
-  for (; b0 + 64 <= b; b0 += 64) before += wave_sum(tree_lane_tiles(p, b0 + lane));
-  const int n = tree_lane_tiles(p, b0 + lane), pre = wave_prefix(n, lane);
+  const TreeShare share = tree_share(p, lane);
+  const int per = share.per;
+  int before = 0, b0 = 0;
+  for (; b0 + 64 <= b; b0 += 64) before += wave_sum(share.padded(tree_lane_tiles(p, b0 + lane)));
+  const int n = share.padded(tree_lane_tiles(p, b0 + lane)), pre = wave_prefix(n, lane);
   const int end = before + __builtin_amdgcn_readlane(pre, b - b0), from = end - __builtin_amdgcn_readlane(n, b - b0);
   first = from / per + b;
   return (end - 1) / per - from / per + 1;
