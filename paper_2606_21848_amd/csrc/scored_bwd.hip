@@ -38,6 +38,14 @@ __device__ __forceinline__ void copy_dword_to_lds(const void* gbase, uint32_t vo
                : "memory", "m0");
 }
 
+// The lane's number, computed anew at each call: what is derived from it is then not kept
+// in registers from one loop iteration to the next.
+__device__ __forceinline__ int lane_again() {
+  unsigned all = ~0u;
+  asm volatile("" : "+s"(all));
+  return (int)__builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0));
+}
+
 // P and dz (times `scale4` / 4 where it is not 1) of one pair: `k` the key, `dp` dP - Dd.
 // shift = C - lse in log2 units.
 template <class Form, bool CAP, bool BIAS>
@@ -469,11 +477,12 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
   const size_t row_bytes = (size_t)p.H * D * 2;
   const unsigned char* gQ = static_cast<const unsigned char*>(p.q) + (size_t)b * p.N * row_bytes;
   const unsigned char* gD = static_cast<const unsigned char*>(p.dout) + (size_t)b * p.N * row_bytes;
-  const TileCopy<D> cp(wave, lane, row_bytes);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)smem;
   // An item's 64 rows' lse, Dd and seen ranges travel with its tiles, 256 bytes each.
   const uint32_t rows0 = lds0 + 4 * T::BYTES;
   auto issue = [&](int i, int stage) {
+    const int lane = lane_again();
+    const TileCopy<D> cp(wave, lane, row_bytes);
     const int h = g * R + i / per, r0 = (first + i % per) * kTileRows;
     const uint32_t st = lds0 + stage * 2 * T::BYTES, rs = rows0 + stage * 1024 + wave * 256;
     cp.issue(gQ + (size_t)h * D * 2, row_bytes, r0, p.N, wave, lane, st);
@@ -486,7 +495,6 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
                                   : static_cast<const void*>(p.row_hi + br);
     copy_dword_to_lds(src, off, rs);
   };
-  const FragOffsets<D> fo(fr, grp);
   it = seek(it);
   int stage = 0;
   if (it < items) issue(it, 0);
@@ -498,7 +506,8 @@ __global__ __launch_bounds__(kThreads, 2) void scored_dv_kernel(ScoredParams p) 
     if (next < items) issue(next, stage ^ 1);
     const int q0 = (first + it % per) * kTileRows, h = g * R + it / per;
     const i32x4 s = bounds(it);
-    const FragOffsets<D> fi = fo.at(lds0 + stage * 2 * T::BYTES);
+    const int lane = lane_again(), fr = lane & 15, grp = lane >> 4;
+    const FragOffsets<D> fi = FragOffsets<D>(fr, grp).at(lds0 + stage * 2 * T::BYTES);
     const int rows_it = (int)(rows0 + stage * 1024);
     it = next;
     stage ^= 1;

@@ -174,28 +174,26 @@ template <int D>
 struct TileCopy {
   using T = AttnTile<D, 64>;
   static constexpr int RPC = 1024 / T::ROW, COPIES = T::COPIES;
-  uint32_t chunk[COPIES];
+  uint32_t chunk;  // of the lane's row, the same for every copy: they lie 16 rows or 32 apart,
+                   // which is a whole period of the swizzle
   uint32_t lane_row;
   __device__ __forceinline__ TileCopy(int wave, int lane, size_t row_bytes)
-      : lane_row((uint32_t)(lane / T::CHUNKS) * (uint32_t)row_bytes) {
-#pragma unroll
-    for (int c = 0; c < COPIES; ++c)
-      chunk[c] = (uint32_t)(T::swz((c * 4 + wave) * RPC + lane / T::CHUNKS, lane % T::CHUNKS) * 16);
-  }
+      : chunk((uint32_t)(T::swz(wave * RPC + lane / T::CHUNKS, lane % T::CHUNKS) * 16)),
+        lane_row((uint32_t)(lane / T::CHUNKS) * (uint32_t)row_bytes) {}
   __device__ __forceinline__ void issue(const unsigned char* g, size_t row_bytes, int row0, int n_rows,
                                         int wave, int lane, uint32_t lds) const {
     if (row0 + 64 <= n_rows) {
       const unsigned char* base = g + (size_t)row0 * row_bytes;
 #pragma unroll
       for (int c = 0; c < COPIES; ++c)
-        copy_to_lds(base + (size_t)((c * 4 + wave) * RPC) * row_bytes, lane_row + chunk[c],
+        copy_to_lds(base + (size_t)((c * 4 + wave) * RPC) * row_bytes, lane_row + chunk,
                     lds + (c * 4 + wave) * 1024);
     } else {
 #pragma unroll
       for (int c = 0; c < COPIES; ++c) {
         const int r0 = row0 + (c * 4 + wave) * RPC, r0c = min(r0, n_rows - 1);
         const int rl = min(r0 + lane / T::CHUNKS, n_rows - 1) - r0c;
-        copy_to_lds(g + (size_t)r0c * row_bytes, (uint32_t)(rl * row_bytes) + chunk[c],
+        copy_to_lds(g + (size_t)r0c * row_bytes, (uint32_t)(rl * row_bytes) + chunk,
                     lds + (c * 4 + wave) * 1024);
       }
     }
