@@ -86,6 +86,15 @@ def test_tree_rejects_bad_arguments(lib):  # noqa: F811
     expect(lib, tree(lib, c=cache(d=96)), kb.KL_ERR_UNSUPPORTED, "d_head 96")
     expect(lib, tree(lib, c=cache(L_max=2 ** 31 - 1)), kb.KL_ERR_UNSUPPORTED, "capacity")
     expect(lib, tree(lib, B=1 << 24, T=64), kb.KL_ERR_UNSUPPORTED, "too large")
+    expect(lib, tree(lib, B=1 << 16, T=4, H=8), kb.KL_ERR_UNSUPPORTED, "too large")
+    expect(lib, tree(lib, c=cache(L_max=1 << 30), B=32, T=1), kb.KL_ERR_UNSUPPORTED, "too large")
+    c = cache(L_max=5000)
+    for B in (2, 9):
+        need = lib.keyless_tree_decode_workspace_size(ctypes.byref(c), B, 4, 8)
+        assert need > 0
+        expect(lib, tree(lib, c=c, B=B, ws_bytes=need - 1), kb.KL_ERR_WORKSPACE, "workspace")
+        expect(lib, tree(lib, c=c, B=B, ws=None), kb.KL_ERR_WORKSPACE, "workspace")
+        expect(lib, tree(lib, c=c, B=B, ws=ODD), kb.KL_ERR_INVALID_ARG, "aligned")
     for x in (-1.0, float("nan"), float("inf")):
         expect(lib, tree(lib, cap=x), kb.KL_ERR_INVALID_ARG, "cap")
         expect(lib, tree(lib, scale=x), kb.KL_ERR_INVALID_ARG, "scale")

@@ -326,3 +326,59 @@ def test_draft_step_graph_replays(lib, dtype):
         for g, vc, out, _ in graphs:
             same = bool(torch.equal(out, want)), bool(torch.equal(vc.data, ref.data))
             assert same == (True, True), f"replay {rep}"
+
+
+# Batches whose rows are shared out evenly over the chip: pieces that cross sequences
+# (many groups, so that a piece is long), pieces that do not, more than 64 sequences (the
+# lanes of a wave) with most of them empty, one or two blocks of 16, 32 and 64 query rows,
+# a last block that is not full, and the last drafted token of 64.
+def _lengths(kind, B, room):
+    rs = np.random.RandomState(B + room)
+    if kind == "even":
+        return [room - 70] * B
+    if kind == "one long":
+        return [room] + [int(x) for x in rs.randint(0, 3, B - 1)]
+    if kind == "last long":
+        return [0] * (B - 1) + [room - 1]
+    return [int(x) for x in rs.randint(0, room + 1, B)]
+
+
+SHARED = [(6, 4, 32, 32, 64, 2400, "uneven"), (5, 3, 32, 32, 128, 1500, "even"), (6, 4, 4, 4, 64, 1700, "uneven"),
+          (9, 1, 12, 2, 128, 1100, "one long"), (70, 2, 2, 2, 64, 1040, "uneven"), (131, 1, 2, 1, 64, 1100, "last long"),
+          (66, 5, 4, 1, 64, 1030, "one long"), (5, 64, 1, 1, 64, 1200, "uneven"), (6, 50, 3, 1, 128, 1100, "uneven"),
+          (5, 16, 16, 4, 64, 1300, "last long"), (5, 9, 12, 4, 128, 1200, "uneven"), (7, 64, 2, 2, 128, 1100, "even")]
+
+
+@pytest.mark.parametrize("layout", ["contiguous", "paged"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,T,H,G,d,room,kind", SHARED)
+def test_shared_out_rows_match_oracle(lib, dtype, layout, B, T, H, G, d, room, kind):
+    say(f"tree, shared rows {dtype} {layout} B={B} T={T} H={H} G={G} d={d} room={room} {kind}")
+    vc, c, table, room = make_cache(dtype, B, G, d, room, layout, 431)
+    n = _lengths(kind, B, room)
+    q = synth.normal((B, T, H, d), 431, 2, 2.0, dtype)
+    words = random_tree(B, T, 432)
+    cap, sl = (25.0, slopes_of(H) * 0.02) if B % 2 else (0.0, None)
+    out = torch.full((B, T, H, d), float("nan"), dtype=dtype, device=DEV)
+    ws = torch.full((kb.tree_decode_workspace_bytes(vc, B, T, H),), 0xFF, dtype=torch.uint8, device=DEV)
+    assert ws.numel() > 0
+    args = (q.to(DEV), vc, gpu(n, torch.int32), gpu(words.view(np.int64)))
+    got = kb.keyless_tree_decode(*args, cap=cap, slopes=gpu(sl), out=out, workspace=ws)
+    again = kb.keyless_tree_decode(*args, cap=cap, slopes=gpu(sl))
+    torch.cuda.synchronize()
+    assert torch.equal(got, again)
+    ref, tol = tree_bound(to64(q), to64(c), n, words, H, G, cap, sl, table, 16, dtype == torch.bfloat16, room)
+    check("tree", to64(got), ref, tol)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_cache_without_room(lib, dtype):
+    """Capacity zero: every token sees nothing, and gets zeros."""
+    say(f"tree, no capacity, {dtype}")
+    B, T, H, G, d = 3, 20, 4, 1, 64
+    vc = kb.ValueCache(torch.full((B, G, 8, d), float("nan"), dtype=dtype, device=DEV))
+    vc.desc.L_max = 0
+    q = synth.normal((B, T, H, d), 433, 2, 1.0, dtype).to(DEV)
+    got = kb.keyless_tree_decode(q, vc, gpu([0, 3, -1], torch.int32))
+    torch.cuda.synchronize()
+    assert not got.any()
