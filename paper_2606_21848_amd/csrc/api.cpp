@@ -1389,10 +1389,24 @@ namespace {
 
 // Work split of a drafted-token decode, from the shapes alone (the kernels share the
 // rows out from the lengths): the workgroups that the chip runs at once, two per CU (one
-// of 64 query rows).
-//  - A capacity of at most 1024 rows is one piece per sequence, without a merge.
-//  - At most kSmallBatch sequences: fixed pieces of at least 128 rows.
-//  - Otherwise even pieces of all rows.
+// of 64 query rows). Times in us, bf16, 32 heads on 8 groups of 128, shorter form first.
+// Query rows per workgroup (bf16; the tokens and heads of a group):
+//  - 16 for up to 16 rows, and where all blocks of 16 have at most 32 tiles for each
+//    workgroup: latency counts there (8 sequences of 500 to 1000 rows, 16 tokens: 12.5
+//    against 21.0 of 64 rows; 1 of 8000: 13.5 against 16.6 of 32 and 17.1 of 64; at 60
+//    tiles, 4 of 8000 rows, 25.8 against 25.0 of 32).
+//  - 32 for up to 32 rows or few (sequence, group) pairs: a workgroup of 64 has its CU to
+//    itself (3 sequences of 30000 rows, 16 tokens: 67.5 against 73.9).
+//  - Else 64, which read a cached row once (8 of 8000: 46.8 against 50.1 of 32).
+// Pieces:
+//  - One per sequence, without a merge, where the capacity is at most 1024 rows, or 2048
+//    and the sequences alone fill the chip (4 tokens, 64 sequences of 400 to 1000 rows:
+//    19.6 against 28.5 of even pieces; of 1000 to 2000: 35.9 against 43.6; 8 of 1900 to
+//    2000, which do not fill it, 24.5 against 15.8).
+//  - At most kSmallBatch sequences: fixed pieces of at least 128 rows (4 sequences of 8000
+//    rows, 16 tokens: 26.6 against 36.0; of 2000 to 16000 rows, 4 tokens: 20.6 against 19.1).
+//  - Otherwise even pieces of all rows (8 of 2000 to 16000 rows: 29.3 against 32.4 of fixed
+//    ones; of 8000 rows each: 31.4 against 28.2).
 struct TreePlan {
   int chunks, least, per, block_rows;
   size_t ml, total;
@@ -1400,13 +1414,15 @@ struct TreePlan {
 TreePlan plan_tree(const kl_value_cache* c, int B, int T, int H) {
   TreePlan pl{};
   const long M = (long)T * (H / c->G), tiles = (cache_capacity(c) + 31) / 32;
-  pl.block_rows = c->dtype != KL_BF16 || M <= 16 ? 16 : M <= 32 ? 32 : 64;
+  const long narrow = (M + 15) / 16 * c->G * B * tiles;  // (block of 16 rows, tile) pairs
+  if (c->dtype != KL_BF16 || M <= 16 || narrow <= 32 * 2 * kComputeUnits) pl.block_rows = 16;
+  else pl.block_rows = M <= 32 || (long)B * c->G <= 32 ? 32 : 64;
   const long blocks = (M + pl.block_rows - 1) / pl.block_rows * c->G;
   const long slots = (pl.block_rows == 64 ? kComputeUnits : 2 * kComputeUnits);
   pl.chunks = 1;
   pl.least = 4;
-  if (tiles <= 32) {
-    pl.per = 32;
+  if (tiles <= 32 || (tiles <= 64 && B * blocks >= slots)) {
+    pl.per = 64;
     return pl;
   }
   if (B <= kSmallBatch) {

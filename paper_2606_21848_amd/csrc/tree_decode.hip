@@ -406,7 +406,9 @@ hipError_t launch_qb(const TreeParams& p, hipStream_t st) {
 template <typename E, int D>
 hipError_t launch_merge(const TreeParams& p, hipStream_t st) {
   const int M = p.T * (p.H / p.G);
-  // Few rows: eight groups of lanes share a row's chunks (batch 1 has many of them).
+  // Few rows: eight groups of lanes share a row's pieces (a batch of one has many of them:
+  // 4 tokens, 30000 rows, 32 heads on 8 groups, 18.0 us in all against 21.7 of one group;
+  // with 1024 rows in 4 sequences 32.8 against 33.1, with 2048 39.0 against 37.9).
   if ((long)p.B * p.G * M <= 1024) {
     constexpr int SUB = 8, ROWS = kThreads / (D / 4) / SUB;
     hipLaunchKernelGGL((tree_merge_kernel<E, D, SUB>), dim3(p.B * p.G * ((M + ROWS - 1) / ROWS)),

@@ -346,22 +346,31 @@ def _lengths(kind, B, room):
 SHARED = [(6, 4, 32, 32, 64, 2400, "uneven"), (5, 3, 32, 32, 128, 1500, "even"), (6, 4, 4, 4, 64, 1700, "uneven"),
           (9, 1, 12, 2, 128, 1100, "one long"), (70, 2, 2, 2, 64, 1040, "uneven"), (131, 1, 2, 1, 64, 1100, "last long"),
           (66, 5, 4, 1, 64, 1030, "one long"), (5, 64, 1, 1, 64, 1200, "uneven"), (6, 50, 3, 1, 128, 1100, "uneven"),
-          (5, 16, 16, 4, 64, 1300, "last long"), (5, 9, 12, 4, 128, 1200, "uneven"), (7, 64, 2, 2, 128, 1100, "even")]
+          (5, 16, 16, 4, 64, 1300, "last long"), (5, 9, 12, 4, 128, 1200, "uneven"), (7, 64, 2, 2, 128, 1100, "even"),
+          # Enough work for workgroups of 32 and 64 query rows: even, fixed and single pieces.
+          (16, 32, 16, 16, 64, 1100, "uneven"), (5, 64, 8, 8, 64, 3400, "uneven"), (6, 40, 16, 8, 64, 3000, "even"),
+          (4, 64, 8, 8, 64, 4200, "uneven"), (4, 60, 16, 16, 64, 2200, "even"), (8, 24, 12, 4, 128, 3100, "uneven"),
+          (9, 64, 8, 8, 64, 2100, "last long")]
+ONE_PIECE = [(32, 48, 8, 8, 64, 1000, "uneven"), (32, 48, 8, 8, 64, 1500, "uneven"), (64, 4, 16, 8, 64, 2000, "one long"),
+             (40, 17, 16, 16, 64, 1040, "uneven")]
 
 
 @pytest.mark.parametrize("layout", ["contiguous", "paged"])
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("B,T,H,G,d,room,kind", SHARED)
+@pytest.mark.parametrize("B,T,H,G,d,room,kind", SHARED + ONE_PIECE)
 def test_shared_out_rows_match_oracle(lib, dtype, layout, B, T, H, G, d, room, kind):
     say(f"tree, shared rows {dtype} {layout} B={B} T={T} H={H} G={G} d={d} room={room} {kind}")
+    one_piece = (B, T, H, G, d, room, kind) in ONE_PIECE
     vc, c, table, room = make_cache(dtype, B, G, d, room, layout, 431)
     n = _lengths(kind, B, room)
     q = synth.normal((B, T, H, d), 431, 2, 2.0, dtype)
     words = random_tree(B, T, 432)
     cap, sl = (25.0, slopes_of(H) * 0.02) if B % 2 else (0.0, None)
     out = torch.full((B, T, H, d), float("nan"), dtype=dtype, device=DEV)
-    ws = torch.full((kb.tree_decode_workspace_bytes(vc, B, T, H),), 0xFF, dtype=torch.uint8, device=DEV)
-    assert ws.numel() > 0
+    need = kb.tree_decode_workspace_bytes(vc, B, T, H)
+    if dtype == torch.bfloat16:
+        assert (need == 0) == one_piece
+    ws = torch.full((max(need, 256),), 0xFF, dtype=torch.uint8, device=DEV)
     args = (q.to(DEV), vc, gpu(n, torch.int32), gpu(words.view(np.int64)))
     got = kb.keyless_tree_decode(*args, cap=cap, slopes=gpu(sl), out=out, workspace=ws)
     again = kb.keyless_tree_decode(*args, cap=cap, slopes=gpu(sl))
@@ -369,6 +378,51 @@ def test_shared_out_rows_match_oracle(lib, dtype, layout, B, T, H, G, d, room, k
     assert torch.equal(got, again)
     ref, tol = tree_bound(to64(q), to64(c), n, words, H, G, cap, sl, table, 16, dtype == torch.bfloat16, room)
     check("tree", to64(got), ref, tol)
+
+
+@pytest.mark.parametrize("B,T,H,G,room", [(6, 64, 8, 8, 2900), (4, 32, 16, 16, 4300), (32, 40, 8, 8, 1024)])
+def test_wide_workgroups_keep_to_seen_rows(lib, B, T, H, G, room):
+    """32 and 64 query rows per workgroup: NaN in a drafted row, past the draft and in blocks
+    that no sequence has; then blocks outside the cache, as if their rows were not there."""
+    d, dtype = 64, torch.bfloat16
+    say(f"tree, wide workgroups, rows not seen B={B} T={T} G={G} room={room}")
+    vc, c, table, room = make_cache(dtype, B, G, d, room, "paged", 434)
+    n = [min(int(x), room - T - 40) for x in np.linspace(3, room, B)]
+    words = random_tree(B, T, 435)
+    words[:, T // 2] |= np.uint64(1 << 2)
+    words[:, T - 1] &= ~np.uint64(1 << 2)
+    q = synth.normal((B, T, H, d), 434, 2, 2.0, dtype).to(DEV)
+    args = (q, vc, gpu(n, torch.int32), gpu(words.view(np.int64)))
+    clean = kb.keyless_tree_decode(*args)
+    torch.cuda.synchronize()
+    data = vc.data.clone()
+    spare = sorted(set(range(c.shape[0])) - set(table.reshape(-1).tolist()))
+    vc.data[spare] = float("nan")
+    for b in range(B):
+        for pos in list(range(n[b] + T, min(n[b] + T + 40, room))) + [n[b] + 2]:
+            vc.data[int(table[b][pos // 16]), :, pos % 16, 5:9] = float("nan")
+    got = kb.keyless_tree_decode(*args)
+    torch.cuda.synchronize()
+    for b in range(B):
+        for t in range(T):
+            if int(words[b][t]) >> 2 & 1:
+                assert not torch.isfinite(got[b, t, :, 5:9]).any()
+            else:
+                assert torch.equal(got[b, t], clean[b, t]), (b, t)
+    # The last sequence without some of its blocks, as a cache of its other rows.
+    vc.data.copy_(data)
+    bad, gone = table.copy(), {B - 1: [1, 7, 8, 40]}
+    for b, blocks in gone.items():
+        bad[b, blocks] = [-1, c.shape[0], 2 ** 31 - 1, -(2 ** 31)]
+    got = kb.keyless_tree_decode(q, kb.ValueCache(vc.data, gpu(bad, torch.int32)), *args[2:])
+    torch.cuda.synchronize()
+    assert torch.equal(got[:B - 1], clean[:B - 1])
+    b = B - 1
+    rows = np.stack([cache_rows(to64(c), b, g, n[b] + T, table) for g in range(G)])
+    keep = np.array([j // 16 not in gone[b] for j in range(n[b] + T)])
+    ref, tol = tree_bound(to64(q)[b:], rows[:, keep][None], [int(keep[:n[b]].sum())], words[b:], H, G, 0.0, None,
+                          None, 16, True, int(keep.sum()))
+    check("tree", to64(got)[b:], ref, tol)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
