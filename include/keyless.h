@@ -431,8 +431,9 @@ int value_cache_append(const kl_value_cache* cache, const void* values,
  *   x_ij = cap tanh(z / cap) - slopes[h] |i - j|      (cap 0: z itself)
  * and row i sees the value rows first[b, i] <= j < last[b, i]. The descriptor lives
  * in host memory; its pointers are device pointers owned by the caller.
- *   cap     >= 0 and finite; 0 for no cap
- *   slopes  [H] fp32, any finite values, or NULL for no bias
+ *   cap     >= 0 and finite; 0 for no cap. bf16: at most 1024 (x is off by up to
+ *           2^-21 cap there); scale / cap at most 1e37
+ *   slopes  [H] fp32, finite, slopes[h] (N - 1) too, or NULL for no bias
  *   first   [B, N] int32, or NULL for 0
  *   last    [B, N] int32, or NULL for i + 1 (causal) or N (not causal); when it is
  *           given, causal is not read
@@ -440,8 +441,8 @@ int value_cache_append(const kl_value_cache* cache, const void* values,
  * A prefix mask: last = max(i + 1, end of the document's prefix). Padding: first =
  * last. Both are clamped to [0, N]; a row with first >= last sees nothing. What a row
  * does not see never reaches it, whatever those values hold (infinities and NaN
- * included); a value that is not finite makes the columns it lies in NaN for every
- * row that sees it.
+ * included); where a row sees a value that is not finite, its result is not finite in
+ * that value's columns at least.
  */
 typedef struct {
   float cap;
@@ -459,8 +460,8 @@ typedef struct {
  * Tensors are 16-byte aligned (lse 4). A row that sees nothing has a zero output and
  * lse = -inf. fp32 sums and softmax statistics; bf16 weights are rounded to bf16 for
  * the weighted sum (the products run on the matrix cores), their sum is not.
- * scale and errors as for keyless_prefill; at most 2^31 - 1 elements per sequence and
- * tensor row counts B * N up to 2^30.
+ * scale (finite) and errors as for keyless_prefill; KL_ERR_UNSUPPORTED from H * d_head =
+ * 2^24 or B * H * ceil(N / 16) = 2^31 on.
  */
 int keyless_scored_forward(const void* q_routed, const void* v, const kl_scoring* scoring, int B,
                            int N, int H, int G, int d_head, float scale, kl_dtype dtype, void* out,
@@ -507,6 +508,8 @@ size_t keyless_scored_backward_workspace_size(int B, int N, int H, int G, int d_
  * a zero row. A row that no token sees is never used, and a row that some tokens do
  * not see never reaches those, whatever it holds. Results do not depend on how the
  * work is split beyond rounding, and are the same from run to run.
+ * KL_ERR_UNSUPPORTED from B * H * T = 2^21 or B * capacity = 2^35 on, and for more than
+ * 2^30 rows of capacity per sequence.
  */
 int keyless_tree_decode(const void* q_routed, const kl_value_cache* cache,
                         const int32_t* lengths_before, const uint64_t* tree, int B, int T, int H,

@@ -1264,15 +1264,28 @@ int keyless_weight_gradients(const void* x, const void* W_Q, const void* W_R, co
 
 namespace {
 
+// The bf16 kernels take cap tanh(z / cap) as cap - 2 cap / (1 + exp(2 z / cap)), whose
+// rounding is up to 2^-21 cap: past a cap of 1024 it would reach the weights' bf16
+// rounding. scale / cap and twice it in log2 units have to be fp32 numbers.
+int check_cap(const char* who, float cap, float scale, kl_dtype dtype) {
+  if (!(cap >= 0.f) || std::isinf(cap))
+    return fail(KL_ERR_INVALID_ARG, "%s: cap must be finite and >= 0 (0 = none)", who);
+  if (cap > 0.f && (double)scale / cap > 1e37)
+    return fail(KL_ERR_UNSUPPORTED, "%s: cap=%g too small for the scale", who, cap);
+  if (dtype == KL_BF16 && cap > 1024.f)
+    return fail(KL_ERR_UNSUPPORTED, "%s: cap=%g (bf16: at most 1024)", who, cap);
+  return KL_OK;
+}
+
 int check_scored_args(const char* who, const void* q, const void* v, const void* out,
                       const kl_scoring* sc, int B, int N, int H, int G, int d_head, kl_dtype dtype,
                       float scale) {
   int s = check_prefill_args(who, q, v, out, B, N, 64, H, G, d_head, dtype, scale);
   if (s != KL_OK) return s;
   if (!sc) return fail(KL_ERR_INVALID_ARG, "%s: scoring is NULL", who);
-  if (!(sc->cap >= 0.f) || std::isinf(sc->cap))
-    return fail(KL_ERR_INVALID_ARG, "%s: cap must be finite and >= 0 (0 = none)", who);
   if (std::isinf(scale)) return fail(KL_ERR_INVALID_ARG, "%s: scale must be finite", who);
+  s = check_cap(who, sc->cap, scale_or_default(scale, d_head), dtype);
+  if (s != KL_OK) return s;
   // Rows of a sequence are addressed with 32-bit byte offsets inside a tile, and the
   // grid holds one workgroup per head and 16 rows at most.
   if ((long)H * d_head >= (1L << 24))
@@ -1464,10 +1477,10 @@ int keyless_tree_decode(const void* q_routed, const kl_value_cache* cache,
     return fail(KL_ERR_UNSUPPORTED, "%s: T=%d drafted tokens (1 to %d)", who, T, kl::kMaxDrafts);
   if (H % cache->G != 0)
     return fail(KL_ERR_INVALID_ARG, "%s: H=%d is not a multiple of G=%d", who, H, cache->G);
-  if (!(cap >= 0.f) || std::isinf(cap))
-    return fail(KL_ERR_INVALID_ARG, "%s: cap must be finite and >= 0 (0 = none)", who);
   if (!(scale >= 0.f) || std::isinf(scale))
     return fail(KL_ERR_INVALID_ARG, "%s: scale must be finite and >= 0 (0 = 1/sqrt(d_head))", who);
+  s = check_cap(who, cap, scale_or_default(scale, cache->d_head), cache->dtype);
+  if (s != KL_OK) return s;
   if (cache_capacity(cache) > (1 << 30))
     return fail(KL_ERR_UNSUPPORTED, "%s: capacity per sequence too large", who);
   // The grid has one workgroup per 16 query rows of a group and piece, 1024 pieces at most.

@@ -129,3 +129,15 @@ def test_binding_checks_shapes_and_types(lib):  # noqa: F811
             kb._like(torch.zeros(shape, dtype=dtype), (2, 2), torch.int32, -1, "first")
     with pytest.raises(ValueError):
         kb._like(torch.zeros((2, 2), dtype=torch.int32), (2, 2), torch.int32, 0, "first")
+
+
+def test_caps_that_fp32_or_bf16_cannot_hold(lib):  # noqa: F811
+    """A cap that overflows scale / cap, and in bf16 one whose rounding would show."""
+    for call in (lambda cap, dt: fwd(lib, sc=desc(cap=cap), dt=dt, N=0),
+                 lambda cap, dt: bwd(lib, sc=desc(cap=cap), dt=dt, N=0),
+                 lambda cap, dt: tree(lib, c=cache(dtype=dt), cap=cap, B=0)):
+        for dt in (kb.KL_BF16, kb.KL_F32):
+            expect(lib, call(1e-39, dt), kb.KL_ERR_UNSUPPORTED, "too small")
+            assert call(1e-30, dt) == call(1024.0, dt) == kb.KL_OK
+        expect(lib, call(1025.0, kb.KL_BF16), kb.KL_ERR_UNSUPPORTED, "at most 1024")
+        assert call(3e38, kb.KL_F32) == kb.KL_OK
