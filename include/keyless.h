@@ -473,9 +473,10 @@ int keyless_scored_forward(const void* q_routed, const void* v, const kl_scoring
  *   dx = P * (dO V^T - rowsum(dO * O)),  P = exp(x - lse)
  *   dz = dx (1 - tanh^2(z / cap))                        (cap 0: dx itself)
  *   dq_routed = scale dz V,   dv = P^T dO + scale dz^T Q~ (summed over a group's heads)
- * out, lse and out_f32 (or NULL) as keyless_scored_forward wrote them for the same
- * arguments; other tensors and the row sums as for keyless_attention_backward. A
- * query row that sees nothing has a zero gradient and gives none. Deterministic (no
+ * out and lse as keyless_scored_forward wrote them for the same arguments, out_f32 too or
+ * NULL (bf16 does not read it: the row sums start from out, and what its rounding takes
+ * from them is added from P and dP on the way); other tensors as for
+ * keyless_attention_backward. A query row that sees nothing has a zero gradient and gives none. Deterministic (no
  * atomics). ws, ws_bytes: keyless_scored_backward_workspace_size(...) bytes, 16-byte
  * aligned; calls that run at the same time must not share it.
  */

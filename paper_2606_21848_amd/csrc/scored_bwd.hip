@@ -93,9 +93,15 @@ __device__ __forceinline__ SeenBounds seen_by_rows(const ScoredParams& p, int b,
   return sb;
 }
 
+// Over a query's four lanes.
+__device__ __forceinline__ float over_groups(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
 // Query row q0 + 16 qb + fr, columns 32 ks + 8 grp .. + 7, of Q~ and dO, what dP starts
-// from (-Dd), and the shift of its scores. Dd comes from the forward's fp32 output when it
-// was kept, else it is there.
+// from (-Dd), and the shift of its scores. Dd comes from the forward's output; correct()
+// makes up for its rounding.
 template <int D, class Form>
 __device__ __forceinline__ void load_query_rows(const ScoredParams& p, const Form& form, int b, int h, int q0,
                                                 int fr, int grp, bf16x8_t (&qf)[QB][D / 32],
@@ -113,22 +119,12 @@ __device__ __forceinline__ void load_query_rows(const ScoredParams& p, const For
           bf16x8_t, *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + at + ks * 32));
       const u32x4 gw = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.dout) + at + ks * 32);
       df[qb][ks] = __builtin_bit_cast(bf16x8_t, gw);
-      if (p.out_f32) {
-        const f32x4_t o0 = *reinterpret_cast<const f32x4_t*>(p.out_f32 + at + ks * 32);
-        const f32x4_t o1 = *reinterpret_cast<const f32x4_t*>(p.out_f32 + at + ks * 32 + 4);
+      const u32x4 o = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.out_in) + at + ks * 32);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          d0 = fmaf(bf16_lo(gw[j]), o0[2 * j], fmaf(bf16_hi(gw[j]), o0[2 * j + 1], d0));
-          d0 = fmaf(bf16_lo(gw[j + 2]), o1[2 * j], fmaf(bf16_hi(gw[j + 2]), o1[2 * j + 1], d0));
-        }
-      }
+      for (int j = 0; j < 4; ++j)
+        d0 = fmaf(bf16_lo(gw[j]), bf16_lo(o[j]), fmaf(bf16_hi(gw[j]), bf16_hi(o[j]), d0));
     }
-    if (p.out_f32) {
-      d0 += __shfl_xor(d0, 16);
-      d0 += __shfl_xor(d0, 32);
-    } else {
-      d0 = p.Dd[row];
-    }
+    d0 = over_groups(d0);
     ndd[qb] = f32x4_t{-d0, -d0, -d0, -d0};
     shift[qb] = form.C() - p.lse[row] * kScoredLog2e;
   }
@@ -234,21 +230,16 @@ __device__ __forceinline__ void dq_step(const Form& form, const FragOffsets<D>& 
         }
 }
 
-// Dd from the forward's output carries the bf16 rounding of the weights there, the same for
-// a whole row: off = sum P (dP - Dd) is what it lacks, and sum P bend V off, taken as
-// (sum P bend) O off (without a cap just that), what dQ~ has too much. Error of dQ~ against
-// 64 bits (8192 tokens, two documents, cap 50): 0.0025 -> 0.0023, of which the roundings of
-// dz and of the result are 0.0016 each.
+// Dd from the forward's output carries the bf16 roundings of that output and of its
+// weights, the same for a whole row: off = sum P (dP - Dd) is what it lacks, and
+// sum P bend V off, taken as (sum P bend) O off (without a cap just that), what dQ~ has too
+// much. Error of dQ~ against 64 bits (8192 tokens, two documents, cap 50): 0.0023, of which
+// the roundings of dz and of the result are 0.0016 each; 0.0025 with the fp32 output and no
+// correction, for 80 us more in 1500.
 __device__ __forceinline__ f32x4_t correct(f32x4_t dq, u32x2 out, float f) {
   return f32x4_t{fmaf(-f, bf16_lo(out[0]), dq[0]), fmaf(-f, bf16_hi(out[0]), dq[1]),
                  fmaf(-f, bf16_lo(out[1]), dq[2]), fmaf(-f, bf16_hi(out[1]), dq[3])};
 }
-// Over a query's four lanes.
-__device__ __forceinline__ float over_groups(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
-}
-
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kThreads, 2) void scored_dq_kernel(ScoredParams p) {
   using T = AttnTile<D, kTileRows>;
@@ -759,10 +750,6 @@ hipError_t launch_d(const ScoredParams& p, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_scored_backward_bf16(const ScoredParams& p, hipStream_t st) {
-  if (!p.out_f32) {  // rowsum(dO * O) from a second forward pass, which has O in fp32
-    const hipError_t e = launch_scored_forward_bf16(p, st);
-    if (e != hipSuccess) return e;
-  }
   return p.D == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);
 }
 

@@ -183,20 +183,6 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p)
     if (q >= p.N) continue;
     const bool none = seen[qb].lo >= seen[qb].hi;
     const float inv = none ? 0.f : 1.f / sum;
-    if (p.Dd) {  // for the backward: rowsum(dO * O), O in fp32, in place of the output
-      const uint16_t* go = static_cast<const uint16_t*>(p.dout) + (((size_t)b * p.N + q) * p.H + h) * D + grp * 4;
-      float d0 = 0.f;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(go + db * 16);
-        d0 = fmaf(bf16_lo(w[0]), o[db][qb][0], fmaf(bf16_hi(w[0]), o[db][qb][1], d0));
-        d0 = fmaf(bf16_lo(w[1]), o[db][qb][2], fmaf(bf16_hi(w[1]), o[db][qb][3], d0));
-      }
-      d0 += __shfl_xor(d0, 16);
-      d0 += __shfl_xor(d0, 32);
-      if (grp == 0) p.Dd[((size_t)b * p.H + h) * p.N + q] = none ? 0.f : d0 * inv;
-      continue;
-    }
     if (p.lse && grp == 0)
       p.lse[((size_t)b * p.H + h) * p.N + q] = none ? -INFINITY : (m[qb] + __log2f(sum)) * kScoredLn2;
     const size_t at = (((size_t)b * p.N + q) * p.H + h) * D + grp * 4;
@@ -330,14 +316,6 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_split_kernel(ScoredPar
     x *= none ? 0.f : 1.f / sum;
     const size_t at = (((size_t)b * p.N + q0 + row) * p.H + h) * D + piece * 4;
     const size_t lrow = ((size_t)b * p.H + h) * p.N + q0 + row;
-    if (p.Dd) {  // for the backward, as in the kernel above; a row's pieces lie in D / 4 lanes
-      const u32x2 w = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p.dout) + at);
-      float d0 = fmaf(bf16_lo(w[0]), x[0], bf16_hi(w[0]) * x[1]);
-      d0 = fmaf(bf16_lo(w[1]), x[2], fmaf(bf16_hi(w[1]), x[3], d0));
-      d0 = group_sum<D / 4>(d0);
-      if (piece == 0) p.Dd[lrow] = d0;
-      continue;
-    }
     if (p.lse && piece == 0) p.lse[lrow] = none ? -INFINITY : (mm + __log2f(sum)) * kScoredLn2;
     if (p.out_f32) *reinterpret_cast<f32x4_t*>(p.out_f32 + at) = x;
     *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
