@@ -221,9 +221,9 @@ constexpr float kLazy = 8.f;  // a softmax reference moves when a score exceeds 
 // The online softmax of QB 16-query blocks over NB 16-row blocks of values: sc holds
 // the dot products on entry (lane: query fr of block qb, rows 16 kb + 4 grp + r of the
 // tile) and the weights on return. `edge` (uniform): some row is not seen by some query,
-// as unseen(qb, kb, r) tells; bias(x, qb, kb, r) takes a pair's bias off; returns whether a pair that is not seen has a product that
-// is not finite (uniform). Its value row is then not finite, and 0 times it would not be
-// either: the caller takes the values that are not finite as zeros, and a query that
+// as unseen(qb, kb, r) tells; bias(x, qb, kb, r) takes a pair's bias off; returns whether a
+// pair that is not seen has a product that is not finite (uniform). Its value row is then
+// not finite, and 0 times it would not be either: the caller takes the values that are not finite as zeros, and a query that
 // sees such a product gets NaN as its score here, and with it as its result.
 template <int D, int NB, int QB, class Form, class Unseen, class Bias>
 __device__ __forceinline__ bool soften(const Form& form, f32x4_t (&sc)[NB][QB], f32x4_t (&o)[D / 16][QB],

@@ -11,7 +11,14 @@
 //
 // The routed queries are not multiplied by the scale (that would round them once
 // more): the scale joins the exponent's multiply-add. The weights' sum is taken from
-// the unrounded weights, in fp32, since the backward pass forms P from it.
+// the unrounded weights, in fp32, since the backward pass forms P from it; the weights are
+// rounded to bf16 once, as the second product's operand.
+//
+// 8192 tokens, 32 heads on 8 groups of 128, causal, cap 50: 615 us, 0.89 PFLOP/s. Matrix
+// instructions take 36% of the cycles and the vector ones of the softmax (an exponential
+// and a reciprocal for the cap, an exponential for the weight) 59%, and the two hardly
+// overlap: an instruction of one wave does not start while the other wave's occupies the
+// issue. Interleaving them by hand spilled 50 registers and more (840 us).
 
 #include <type_traits>
 
@@ -197,7 +204,8 @@ __global__ __launch_bounds__(kThreads, 2) void scored_fwd_kernel(ScoredParams p)
 
 // The same for few query tiles (short prompts, few heads): a workgroup owns 32 query rows
 // of one head and its four waves share the 32-row value tiles, tile t to wave t % 4, each
-// through a private two-stage ring with no barrier, and meet once to merge.
+// through a private two-stage ring with no barrier, and meet once to merge. 517 tokens, 12
+// heads, prefix mask, cap 30: 10.2 us, the latency of a few tiles and of the merge.
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kThreads, 2) void scored_fwd_split_kernel(ScoredParams p) {
   constexpr int QB = 2, NW = 4, RV = 32, BQ = 16 * QB, KS = D / 32, DB = D / 16;
