@@ -567,6 +567,13 @@ def _like(t, shape, dtype, dev, what):
     raise ValueError(f"{what} must be contiguous")
 
 
+def _workspace(t: torch.Tensor, dev: int):
+    """(address, bytes) of a workspace on that device."""
+    if t.get_device() != dev:
+        raise ValueError("the workspace is on another device than the first argument")
+    return _ptr(t), t.numel() * t.element_size()
+
+
 def _call(dev: int, fn, *args):
     """fn on that device's current stream, whichever device is current."""
     if dev == torch._C._cuda_getDevice():
@@ -646,8 +653,7 @@ def keyless_scored_backward(q_routed: torch.Tensor, v: torch.Tensor, out: torch.
           _like(out, like_q, dt, dev, "out"), _like(out_f32, like_q, torch.float32, dev, "out_f32"),
           _like(dout, like_q, dt, dev, "dout"), _like(lse, (B, H, N), torch.float32, dev, "lse"),
           scoring.checked(B, N, H, dev), B, N, H, G, dk, scale, _dt(q_routed),
-          _like(dq, like_q, dt, dev, "dq"), _like(dv, (B, N, G, dk), dt, dev, "dv"), _ptr(workspace),
-          workspace.numel() * workspace.element_size())
+          _like(dq, like_q, dt, dev, "dq"), _like(dv, (B, N, G, dk), dt, dev, "dv"), *_workspace(workspace, dev))
     return dq, dv
 
 
@@ -660,6 +666,8 @@ def _per_sequence(cache: ValueCache, t: torch.Tensor, B: int, dev: int, what: st
     rows = cache.data if cache.block_table is None else cache.block_table
     if rows.shape[0] != B:
         raise ValueError(f"the cache holds {rows.shape[0]} sequences, not {B}")
+    if cache.data.get_device() != dev or rows.get_device() != dev:
+        raise ValueError("the cache is on another device than the first argument")
     return _like(t, (B,), torch.int32, dev, what)
 
 
@@ -685,8 +693,7 @@ def keyless_tree_decode(q_routed: torch.Tensor, cache: ValueCache, lengths_befor
           _per_sequence(cache, lengths_before, B, dev, "lengths_before"),
           _like(tree, (B, T), torch.int64, dev, "tree"), B, T, H, cap,
           _like(slopes, (H,), torch.float32, dev, "slopes"), scale,
-          _like(out, like_q, dt, dev, "out"), _ptr(workspace),
-          workspace.numel() * workspace.element_size())
+          _like(out, like_q, dt, dev, "out"), *_workspace(workspace, dev))
     return out
 
 

@@ -1310,7 +1310,7 @@ ScoredBwdLayout scored_bwd_layout(int B, int N, int H, int G, int d_head, kl_dty
   L.hi = L.lo + align256((size_t)B * N * sizeof(int));
   L.tiles = L.hi + align256((size_t)B * N * sizeof(int));
   L.splits = L.tiles + align256((size_t)B * ((N + tile - 1) / tile) * 4 * sizeof(int));
-  L.part = L.splits + align256((size_t)B * ((N + 191) / 192) * sizeof(int));
+  L.part = L.splits + align256((size_t)B * ((N + 191L) / 192) * sizeof(int));
   L.total = L.part + (L.S > 1 ? align256((size_t)L.S * B * N * G * d_head * sizeof(float)) : 0);
   return L;
 }

@@ -3,6 +3,7 @@ the cache's keep, without a GPU: every call fails host-side validation (or has n
 to do), so nothing is launched."""
 
 import ctypes
+import types
 
 import pytest
 import torch
@@ -141,3 +142,15 @@ def test_caps_that_fp32_or_bf16_cannot_hold(lib):  # noqa: F811
             assert call(1e-30, dt) == call(1024.0, dt) == kb.KL_OK
         expect(lib, call(1025.0, kb.KL_BF16), kb.KL_ERR_UNSUPPORTED, "at most 1024")
         assert call(3e38, kb.KL_F32) == kb.KL_OK
+
+
+def test_binding_refuses_another_device():
+    """A cache or a workspace that is not where the first argument is."""
+    here = types.SimpleNamespace(data=torch.zeros((2, 1, 8, 64)), block_table=None)
+    n = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="another device"):
+        kb._per_sequence(here, n, 2, 0, "lengths_before")
+    with pytest.raises(ValueError, match="2 sequences"):
+        kb._per_sequence(here, n, 3, -1, "lengths_before")
+    with pytest.raises(ValueError, match="another device"):
+        kb._workspace(torch.zeros(256, dtype=torch.uint8), 0)
