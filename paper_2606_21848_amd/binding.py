@@ -165,6 +165,7 @@ class ValueCache:
     def __init__(self, data: torch.Tensor, block_table: torch.Tensor | None = None):
         self.data = data
         self.block_table = block_table
+        self.dev = data.get_device()
         d = KLValueCache()
         d.data = data.data_ptr()
         d.dtype = _dt(data)
@@ -177,6 +178,8 @@ class ValueCache:
             if block_table.dtype != torch.int32:
                 raise TypeError("block_table must be int32")
             _ptr(block_table)
+            if block_table.get_device() != self.dev:
+                raise ValueError("block_table is on another device than the cache")
             d.layout = KL_PAGED
             d.block_size = data.shape[2]
             d.num_blocks = data.shape[0]
@@ -666,7 +669,7 @@ def _per_sequence(cache: ValueCache, t: torch.Tensor, B: int, dev: int, what: st
     rows = cache.data if cache.block_table is None else cache.block_table
     if rows.shape[0] != B:
         raise ValueError(f"the cache holds {rows.shape[0]} sequences, not {B}")
-    if cache.data.get_device() != dev or rows.get_device() != dev:
+    if cache.dev != dev:
         raise ValueError("the cache is on another device than the first argument")
     return _like(t, (B,), torch.int32, dev, what)
 

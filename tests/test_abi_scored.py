@@ -146,7 +146,7 @@ def test_caps_that_fp32_or_bf16_cannot_hold(lib):  # noqa: F811
 
 def test_binding_refuses_another_device():
     """A cache or a workspace that is not where the first argument is."""
-    here = types.SimpleNamespace(data=torch.zeros((2, 1, 8, 64)), block_table=None)
+    here = types.SimpleNamespace(data=torch.zeros((2, 1, 8, 64)), block_table=None, dev=-1)
     n = torch.zeros(2, dtype=torch.int32)
     with pytest.raises(ValueError, match="another device"):
         kb._per_sequence(here, n, 2, 0, "lengths_before")
