@@ -351,3 +351,47 @@ def test_a_long_sequence_by_rows(lib):
             ref_dv[k] += p @ g64[sees, h] + tau * (dz @ q64[sees, h])
     got = to64(dv)[0, list(rows), 0]
     assert np.linalg.norm(got - ref_dv) <= 3 * 2.0 ** -8 * np.linalg.norm(ref_dv)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bias", [False, True])
+def test_the_largest_cap(lib, dtype, bias):
+    """A cap of 1024, the most that bf16 takes: nearly straight scores, formed as a small
+    difference of large numbers."""
+    B, N, H, G, d = 1, 210, 4, 2, 128
+    say(f"scored, cap 1024, bias {bias}, {dtype}")
+    q, v, g = case(dtype, B, N, H, G, d, 331)
+    sc, sl, seen = scoring("docs", B, N, H, 1024.0, bias)
+    args = [to64(x) for x in (q, v, g)]
+    tol = bounds(*args, 1024.0, sl, seen, dtype == torch.bfloat16)
+    q, v, g = q.to(DEV), v.to(DEV), g.to(DEV)
+    out, lse = kb.keyless_scored_forward(q, v, sc)
+    dq, dv = kb.keyless_scored_backward(q, v, out, g, lse, sc)
+    torch.cuda.synchronize()
+    ref, ref_lse = S.scored_attention(*args[:2], 1024.0, sl, seen)
+    check("out", to64(out), ref, tol["out"])
+    check("lse", to64(lse), ref_lse, tol["lse"])
+    for got, r, k in zip((dq, dv), S.scored_attention_backward(*args, 1024.0, sl, seen), ("dq", "dv")):
+        check(k, to64(got), r, tol[k])
+
+
+def test_the_kept_fp32_output_changes_nothing_in_bf16(lib):
+    """The row sums of the bf16 backward start from the output alone, and what its rounding
+    takes from them is added on the way: dQ~ is about as exact as its own rounding, sqrt(2)
+    of it with that of dz, and so below 1.6 of it."""
+    B, N, H, G, d = 1, 700, 4, 2, 128
+    say("scored, fp32 output kept and not")
+    q, v, g = case(torch.bfloat16, B, N, H, G, d, 332)
+    args = [to64(x) for x in (q, v, g)]
+    q, v, g = q.to(DEV), v.to(DEV), g.to(DEV)
+    for cap in (0.0, 5.0, 50.0):
+        sc, sl, seen = scoring("causal", B, N, H, cap, False)
+        o32 = torch.empty(q.shape, dtype=torch.float32, device=DEV)
+        out, lse = kb.keyless_scored_forward(q, v, sc, out_f32=o32)
+        a = kb.keyless_scored_backward(q, v, out, g, lse, sc)
+        b = kb.keyless_scored_backward(q, v, out, g, lse, sc, out_f32=o32)
+        torch.cuda.synchronize()
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        ref = S.scored_attention_backward(*args, cap, sl, seen)[0]
+        own = torch.from_numpy(ref).to(torch.bfloat16).double().numpy()
+        assert np.linalg.norm(to64(a[0]) - ref) <= 1.6 * np.linalg.norm(own - ref)
